@@ -188,8 +188,7 @@ def _handle(s):
         tokens = np.add.reduceat(en - st, off[:-1]).astype(np.int64)
         return span.prepare_paged_span_decode_attn(s["q"], *cache, *s["span"], s["scale"], weights=s.get("weights"), tokens_per_seq=tokens)
     if c["op"] == "decode":
-        return span.prepare_paged_decode_attn(s["q"], *cache, s["lens"], s["scale"], window=c["window"], sinks=c["sinks"], weights=s.get("weights"),
-                                              tokens_per_seq=s["lens_host"])
+        return span.prepare_paged_decode_attn(s["q"], *cache, s["lens"], s["scale"], window=c["window"], sinks=c["sinks"], weights=s.get("weights"))
     if c["op"] == "prompt":
         return span.prepare_paged_prompt_attn(s["q"], *cache, s["lens"], s["offsets"], s["scale"], window=c["window"], sinks=c["sinks"])
     return span.prepare_paged_evict(*cache, s["lens"], s["weights"], c["budget"], positions=s["positions"], sinks=c["sinks"], recent=c["recent"],
