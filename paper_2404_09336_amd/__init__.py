@@ -12,3 +12,8 @@ from .binding import (  # noqa: F401
     span_validate, span_build, span_blocks_to_intervals, span_intervals_to_blocks,
     span_plan_query, span_launch_query, span_workspace_bytes, span_workspace_init, span_strerror,
 )
+from .paged import (  # noqa: F401
+    paged_append, prepare_paged_append, paged_decode_attn, prepare_paged_decode_attn,
+    paged_span_decode_attn, prepare_paged_span_decode_attn, paged_evict, prepare_paged_evict,
+    paged_workspace_bytes, paged_workspace_init,
+)

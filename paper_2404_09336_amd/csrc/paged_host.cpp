@@ -1,0 +1,125 @@
+// Host-only parts of the operators on a cache in pages: argument checks, slices, workspaces.  No GPU call in this file.
+#include <limits.h>
+
+#include <algorithm>
+
+#include "paged_internal.h"
+
+namespace spanattn {
+
+int check_paged(const span_paged_desc_t* d) {
+  if (!d) return SPAN_ERR_NULL;
+  if (d->batch <= 0 || d->batch > 65535 || d->heads <= 0 || d->kv_heads <= 0 || d->kv_heads > 65535) return SPAN_ERR_SHAPE;
+  if (d->heads % d->kv_heads != 0 || d->heads / d->kv_heads > kMaxGroup) return SPAN_ERR_SHAPE;
+  if (d->head_dim != 64 && d->head_dim != 128) return SPAN_ERR_SHAPE;
+  if (d->page_size < 16 || d->page_size > 1024 || (d->page_size & (d->page_size - 1)) != 0) return SPAN_ERR_SHAPE;
+  if (d->num_pages <= 0 || (int64_t)d->num_pages * d->page_size > INT_MAX) return SPAN_ERR_SHAPE;
+  if (d->table_pages <= 0 || (int64_t)d->table_pages * d->page_size > kMaxLen) return SPAN_ERR_SHAPE;
+  if ((int64_t)d->batch * d->heads > INT_MAX / 2) return SPAN_ERR_SHAPE;
+  if (d->num_tokens < 0 || d->window < 0 || d->sinks < 0 || d->num_intervals < 0 || d->num_splits < 0 || d->budget < 0 || d->recent < 0)
+    return SPAN_ERR_SHAPE;
+  if (d->dtype != SPAN_F32 && d->dtype != SPAN_F16 && d->dtype != SPAN_BF16) return SPAN_ERR_DTYPE;
+  return SPAN_OK;
+}
+
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+static int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// Workgroups a one-token call aims at.
+constexpr int64_t kPagedWorkgroups = 1024;
+
+static int64_t slice_room(const span_paged_desc_t* d) { return std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads); }
+
+PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
+  PagedPlan p = {0, 1, false, 0};
+  const int64_t cap = capacity(d), room = slice_room(d);
+  auto uniform = [&](int64_t splits) {
+    splits = std::min(splits, ceil_div(cap, kPagedSliceStep));
+    splits = std::min<int64_t>(splits, 65535 / d->batch);  // grid.y
+    p.splits = (int32_t)std::max<int64_t>(splits, 1);
+    p.rows = p.splits * d->batch;
+    return p;
+  };
+  if (d->num_splits > 0) return uniform(d->num_splits);
+  if (!spans) {
+    if (d->batch > kPagedLocateBatch) return uniform(1);
+    const int64_t most = d->window > 0 ? std::min<int64_t>(cap, (int64_t)d->window + d->sinks) : cap;  // positions of any sequence
+    if (most <= kPagedLeastSlice) return uniform(1);
+    p.room = (int32_t)room;
+    p.splits = 2;
+    p.rows = (int32_t)std::min<int64_t>(room + d->batch, ceil_div(most, kPagedLeastSlice) * d->batch);
+    return p;
+  }
+  if (d->tokens_per_seq && d->batch <= kMaxPlanSlices) {
+    auto tokens = [&](int32_t b) { return std::min(std::max<int64_t>(d->tokens_per_seq[b], 0), cap); };
+    int64_t sum = 0;
+    for (int32_t b = 0; b < d->batch; ++b) sum += tokens(b);
+    // at most room + batch slices; the table's entries bound them
+    const int64_t aim = std::max<int64_t>(1, std::min<int64_t>(room, kMaxPlanSlices - d->batch));
+    const int64_t T = std::max<int64_t>(kPagedLeastSlice, round_up(ceil_div(sum, aim), kPagedSliceStep));
+    int64_t most = 1, least = kMaxPlanSplits, y = 0;
+    for (int32_t b = 0; b < d->batch; ++b) {
+      const int64_t nsl = std::max<int64_t>(1, ceil_div(tokens(b), T));
+      most = std::max(most, nsl);
+      least = std::min(least, nsl);
+      y += nsl;
+    }
+    if (most == least) return uniform(most);
+    if (y <= kMaxPlanSlices && most <= kMaxPlanSplits) {
+      if (table) {
+        int32_t at = 0;
+        for (int32_t b = 0; b < d->batch; ++b) {
+          const int64_t nsl = std::max<int64_t>(1, ceil_div(tokens(b), T));
+          for (int64_t s = 0; s < nsl; ++s) table[at++] = pack_slice((uint32_t)b, (uint32_t)s, (uint32_t)nsl);
+        }
+      }
+      p.table = true;
+      p.splits = (int32_t)most;
+      p.rows = (int32_t)y;
+      return p;
+    }
+  }
+  return uniform(std::min(ceil_div(room, d->batch), ceil_div(cap, kPagedLeastSlice)));
+}
+
+PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights) {
+  PagedWorkspace w = {};
+  w.sliced = p.splits > 1;
+  w.weights = weights;
+  w.spans = spans;
+  const size_t group = (size_t)(d->heads / d->kv_heads), states = (size_t)p.rows * d->kv_heads * group, cap = (size_t)capacity(d);
+  size_t at = 0;
+  auto part = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  if (w.sliced || weights) part((size_t)d->batch * d->kv_heads * sizeof(int32_t));  // ticket counters, in every call's place for them
+  w.ml = part(w.sliced ? states * 2 * sizeof(float) : 0);
+  w.acc = part(w.sliced ? states * (size_t)d->head_dim * sizeof(float) : 0);
+  w.final_ml = part(weights ? (size_t)d->batch * d->heads * 2 * sizeof(float) : 0);
+  w.counts = part(weights && spans ? (size_t)d->batch * sizeof(int32_t) : 0);
+  w.list = part(weights && spans ? (size_t)d->batch * cap * sizeof(int32_t) : 0);
+  w.scores = part(weights ? (size_t)d->batch * d->heads * cap * sizeof(float) : 0);
+  w.total = at;
+  return w;
+}
+
+// Of every (sequence, KV head) the number of rows that move and their slots, from and to.
+size_t evict_workspace(const span_paged_desc_t* d) {
+  const size_t most = (size_t)std::min(d->budget, std::max(capacity(d) - d->budget, 0));
+  return (((size_t)d->batch * d->kv_heads * (1 + 2 * most) * sizeof(int32_t)) + 255) & ~(size_t)255;
+}
+
+}  // namespace spanattn
+
+extern "C" int paged_check(const span_paged_desc_t* desc) { return spanattn::check_paged(desc); }
+
+extern "C" size_t paged_workspace_bytes(const span_paged_desc_t* desc, int use) {
+  using namespace spanattn;
+  if (check_paged(desc) != SPAN_OK) return 0;
+  if (use == PAGED_EVICT) return evict_workspace(desc);
+  if (use < PAGED_DECODE || use > PAGED_SPAN_DECODE_WEIGHTS) return 0;
+  const bool spans = use >= PAGED_SPAN_DECODE;
+  return paged_workspace(desc, plan_paged(desc, spans, nullptr), spans, (use & 1) != 0).total;
+}

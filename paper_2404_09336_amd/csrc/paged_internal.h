@@ -1,0 +1,41 @@
+// Shared by the translation units of the operators on a cache in pages.
+#ifndef PAGED_INTERNAL_H_
+#define PAGED_INTERNAL_H_
+
+#include "span_internal.h"
+#include "span_paged.h"
+
+namespace spanattn {
+
+constexpr int kMaxGroup = 16;          // query heads per KV head: columns of one 16x16 MFMA
+constexpr int kPagedSliceStep = 32;    // slices are multiples of this many positions (whole tiles, whole quads of scores)
+constexpr int kPagedLeastSlice = 128;  // do not cut finer: a tile per wave
+// Dense calls find their slices on the device, from the lengths, every workgroup for itself (locate_slice); beyond this batch that
+// takes longer than it gains, and there are workgroups enough without slices.
+constexpr int kPagedLocateBatch = 512;
+
+int check_paged(const span_paged_desc_t* d);
+
+inline int page_shift(const span_paged_desc_t* d) { return __builtin_ctz((unsigned)d->page_size); }
+inline int32_t capacity(const span_paged_desc_t* d) { return d->table_pages * d->page_size; }  // positions of a sequence's table
+
+// How a one-token call is cut.
+struct PagedPlan {
+  int32_t room;      // > 0: slices per head the kernel aims at over all sequences (locate_slice), rows = room + batch
+  int32_t splits;    // room 0: slices of every sequence, or the most of any (table)
+  bool table;        // slices from a table of pack_slice entries
+  int32_t rows;      // grid.y: slices of all sequences (upper bound)
+};
+// `table` (kMaxPlanSlices entries) may be null to only size the plan.
+PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table);
+
+// Parts of the workspace of a one-token call, in bytes from its start.
+struct PagedWorkspace {
+  size_t ml, acc, final_ml, counts, list, scores, total;  // counters lie at 0
+  bool sliced, weights, spans;
+};
+PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights);
+size_t evict_workspace(const span_paged_desc_t* d);
+
+}  // namespace spanattn
+#endif

@@ -26,6 +26,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
+extern thread_local int g_last_hip_error;  // the last failed HIP call's, for span_last_hip_error
+
 constexpr int kThreads = kWavesPerBlock * 64;
 constexpr int kWin = 256;  // rows of a wave whose positions are tabulated at a time (one LDS window)
 
@@ -482,6 +484,26 @@ struct GroupMerge {
     }
   }
 };
+
+// The value is computed here and not later: the compiler would otherwise sink the additions below the next tile's loads,
+// and keep all their operands in registers across them.
+__device__ __forceinline__ void pin(f32x4& v) { asm volatile("" : "+v"(v)); }
+
+// `from` of the lane eight further (within its 16) in the lanes of `kBanks` (0x3: lanes 0 - 7 of each 16, 0xc: 8 - 15), `keep` in
+// the others.
+template <int kBanks>
+__device__ __forceinline__ uint32_t swap_half(uint32_t keep, uint32_t from) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)keep, (int)from, 0x128, 0xf, kBanks, false);  // row_ror:8
+}
+
+// 16 bytes to / from memory that all XCDs share (sc1: written through, never served from a stale L2 line).
+constexpr int kThrough = 16;
+__device__ __forceinline__ void publish4(__amdgpu_buffer_rsrc_t slot, uint32_t byte_off, f32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), slot, byte_off, 0, kThrough);
+}
+__device__ __forceinline__ f32x4 observe4(__amdgpu_buffer_rsrc_t slot, uint32_t byte_off) {
+  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slot, byte_off, 0, kThrough));
+}
 
 // Merge two un-normalised softmax states held in log2 units.
 __device__ __forceinline__ void merge_state(float& m, float& l, float* acc, int n, float m2, float l2,

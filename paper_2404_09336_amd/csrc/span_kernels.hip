@@ -37,6 +37,8 @@
 #include "span_matrix.h"
 
 namespace spanattn {
+
+thread_local int g_last_hip_error = 0;
 namespace {
 
 // ---- the streaming kernel ------------------------------------------------------------------------
@@ -592,7 +594,6 @@ __global__ __launch_bounds__(64) void advance_kernel(int max_len, int num_interv
   }
 }
 
-thread_local int g_last_hip_error = 0;
 #ifdef SPAN_PHASE_TRACE
 unsigned long long* g_trace = nullptr;  // set by span_debug_set_trace
 size_t g_trace_workgroups = 0;

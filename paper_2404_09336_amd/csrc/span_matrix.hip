@@ -76,26 +76,6 @@ constexpr int weight_terms(bool two_tokens) {
   return std::is_same<Elt, F16>::value && D == 128 && !two_tokens ? 2 : 3;
 }
 
-// The value is computed here and not later: the compiler would otherwise sink the additions below the next tile's loads,
-// and keep all their operands in registers across them.
-__device__ __forceinline__ void pin(f32x4& v) { asm volatile("" : "+v"(v)); }
-
-// `from` of the lane eight further (within its 16) in the lanes of `kBanks` (0x3: lanes 0 - 7 of each 16, 0xc: 8 - 15), `keep` in
-// the others.
-template <int kBanks>
-__device__ __forceinline__ uint32_t swap_half(uint32_t keep, uint32_t from) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)keep, (int)from, 0x128, 0xf, kBanks, false);  // row_ror:8
-}
-
-// 16 bytes to / from memory that all XCDs share (sc1: written through, never served from a stale L2 line).
-constexpr int kThrough = 16;
-__device__ __forceinline__ void publish4(__amdgpu_buffer_rsrc_t slot, uint32_t byte_off, f32x4 v) {
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), slot, byte_off, 0, kThrough);
-}
-__device__ __forceinline__ f32x4 observe4(__amdgpu_buffer_rsrc_t slot, uint32_t byte_off) {
-  return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(slot, byte_off, 0, kThrough));
-}
-
 // kShared: several workgroups (query blocks) read the same rows, so the rows are loaded with the default cache policy and
 // the later readers find them in the L2; otherwise every row is used once and streams past it.  Inputs that no cache
 // holds from call to call: 32 pairs x ~5500 positions, 20 tokens 29.6 -> 25.2 us; 96 pairs x ~900, 60 tokens 30.1 -> 26.5; 32 pairs
