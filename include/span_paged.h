@@ -118,6 +118,17 @@ int paged_span_decode_attn(const span_paged_desc_t* desc, const void* q, const v
                            const int32_t* span_ends, float scale, float* weights, float* out);
 
 /*
+ * Attention of all new tokens of every sequence (their rows already appended): a prompt, or a chunk of one behind a cached
+ * beginning.  The token at position p sees the positions j <= p with j > p - window (all for window 0) or j < sinks.
+ *   q   : device, desc->dtype, [num_tokens, heads, head_dim]
+ *   out : device, desc->dtype, [num_tokens, heads, head_dim]: it goes on as an activation, in the type those have
+ * Scores, maxima and sums are fp32; a weight of a 16-bit call is rounded to the storage type before it meets V, as the
+ * output is after it.  A token that sees nothing (more new tokens than positions) gets a row of zeros.
+ */
+int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages,
+                      const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, float scale, void* out);
+
+/*
  * Cuts every cache of more than desc->budget rows down to it, for every KV head by itself.  The rows that stay are those of
  * the first `sinks` positions, of the last `recent` (up to the largest position held), and of the others those with the
  * largest weights; of equal weights the lower slot stays, and a NaN weight counts as less than any other.  sinks + recent

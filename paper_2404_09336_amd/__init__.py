@@ -14,6 +14,6 @@ from .binding import (  # noqa: F401
 )
 from .paged import (  # noqa: F401
     paged_append, prepare_paged_append, paged_decode_attn, prepare_paged_decode_attn,
-    paged_span_decode_attn, prepare_paged_span_decode_attn, paged_evict, prepare_paged_evict,
+    paged_span_decode_attn, prepare_paged_span_decode_attn, paged_prompt_attn, prepare_paged_prompt_attn, paged_evict, prepare_paged_evict,
     paged_workspace_bytes, paged_workspace_init,
 )

@@ -13,7 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspanattn.so")
-SOURCES = [os.path.join(CSRC, name) for name in ("span_kernels.hip", "span_matrix.hip", "paged_decode.hip", "paged_cache.hip",
+SOURCES = [os.path.join(CSRC, name) for name in ("span_kernels.hip", "span_matrix.hip", "paged_decode.hip", "paged_cache.hip", "paged_prompt.hip",
                                                  "span_host.cpp", "paged_host.cpp")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # keep the compiler from forming packed-fp32 instructions

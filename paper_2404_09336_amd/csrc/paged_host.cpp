@@ -105,6 +105,32 @@ PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, b
   return w;
 }
 
+// Workgroups from which on a prompt call's tiles are not shared out, and that it aims at where they are.
+constexpr int64_t kPromptFewTiles = 256, kPromptWorkgroups = 512;
+constexpr int64_t kPromptLeastPositions = 256;  // of a share
+
+PromptPlan plan_prompt(const span_paged_desc_t* d) {
+  PromptPlan p;
+  const int32_t group = d->heads / d->kv_heads;
+  p.tokens = kPromptTileRows / group;
+  // each sequence has at most one tile that is not full
+  p.tiles = (int64_t)d->num_tokens / p.tokens + std::min(d->batch, d->num_tokens);
+  const int64_t workgroups = p.tiles * d->kv_heads;
+  int64_t most = capacity(d);
+  if (d->window > 0) most = std::min<int64_t>(most, (int64_t)d->window + d->sinks + p.tokens);
+  int64_t splits = 1;
+  if (workgroups > 0 && workgroups < kPromptFewTiles) splits = std::min(kPromptWorkgroups / workgroups, ceil_div(most, kPromptLeastPositions));
+  p.splits = (int32_t)std::max<int64_t>(splits, 1);
+  const size_t rows = p.splits > 1 ? (size_t)workgroups * p.splits * kPromptTileRows : 0;
+  p.acc = (rows * 2 * sizeof(float) + 255) & ~(size_t)255;
+  return p;
+}
+
+size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p) {
+  if (p.splits == 1) return 0;
+  return p.acc + (size_t)p.tiles * d->kv_heads * p.splits * kPromptTileRows * d->head_dim * sizeof(float);
+}
+
 // Of every (sequence, KV head) the number of rows that move and their slots, from and to.
 size_t evict_workspace(const span_paged_desc_t* d) {
   const size_t most = (size_t)std::min(d->budget, std::max(capacity(d) - d->budget, 0));
@@ -119,6 +145,7 @@ extern "C" size_t paged_workspace_bytes(const span_paged_desc_t* desc, int use) 
   using namespace spanattn;
   if (check_paged(desc) != SPAN_OK) return 0;
   if (use == PAGED_EVICT) return evict_workspace(desc);
+  if (use == PAGED_PROMPT) return prompt_workspace(desc, plan_prompt(desc));
   if (use < PAGED_DECODE || use > PAGED_SPAN_DECODE_WEIGHTS) return 0;
   const bool spans = use >= PAGED_SPAN_DECODE;
   return paged_workspace(desc, plan_paged(desc, spans, nullptr), spans, (use & 1) != 0).total;

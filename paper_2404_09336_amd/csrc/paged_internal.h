@@ -35,6 +35,18 @@ struct PagedWorkspace {
   bool sliced, weights, spans;
 };
 PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights);
+
+// How a prompt call is cut: query rows in tiles, and a tile's positions among several workgroups where there are few tiles.
+constexpr int kPromptTileRows = 128;
+struct PromptPlan {
+  int32_t tokens;   // of a tile: as many as their heads' rows fit
+  int32_t splits;
+  int64_t tiles;    // the most that any offsets give
+  size_t acc;       // bytes of the workspace ahead of the partial outputs
+};
+PromptPlan plan_prompt(const span_paged_desc_t* d);
+size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p);
+
 size_t evict_workspace(const span_paged_desc_t* d);
 
 }  // namespace spanattn

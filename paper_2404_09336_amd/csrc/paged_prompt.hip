@@ -1,0 +1,584 @@
+// Attention of many new tokens per sequence over a cache in pages: causal, with an optional window and sinks, on the matrix cores.
+//
+// A workgroup of 4 wavefronts takes a tile of up to 128 query rows of one KV head - the rows are (token, query head of the group), so the heads
+// that share K and V share a pass over them - and walks the cache in tiles of 64 positions (32 of fp32 rows).  Lane (c, h) = (lane % 32, lane / 32)
+// plays row / column c and contraction half h of the 32x32 MFMAs; a wave has 32 query rows, which are columns throughout:
+//   * scores S^T = K Q^T: Q stays in registers, K comes from LDS.  Lane (c, h) ends up with the scores of query c against positions
+//     8 (r / 4) + 4 h + r % 4 of each 32, r = 0 .. 15, so a maximum or a sum is the lane's own but for one exchange of halves;
+//   * outputs O^T = V^T P^T: the contraction may take the positions in any order as long as both operands do.  The order is the one the scores
+//     lie in, so weights go from the registers that hold them straight into the operand; V is laid down in LDS transposed, with
+//     the positions of 16 in that order, and is read like K.
+// The next tile's rows are on their way to registers while this one is computed, and go to the other half of LDS after it: one barrier per tile.
+// A row of K or V past the sequence's length is not read (the buffer descriptor of a page ends there) and counts as zeros.
+#include "paged_device.h"
+
+namespace spanattn {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPromptWaves = 4, kPromptThreads = 64 * kPromptWaves;
+constexpr int kPromptRows = kPromptTileRows;
+static_assert(kPromptRows == 32 * kPromptWaves, "32 query rows a wave");
+
+struct PromptArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  const int32_t* block_table;
+  const int32_t* ctx_lens;
+  const int32_t* q_offsets;
+  float* part_ml;   // [slots, kPromptRows, 2]; slot = (tile * kv_heads + head) * splits + split
+  float* part_acc;  // [slots, kPromptRows, D]
+  int32_t batch, kv_heads, group, table_pages, page_shift, num_pages, num_tokens, max_len;
+  int32_t tokens;   // of a tile: kPromptRows / group
+  int32_t tiles;    // grid.y
+  int32_t splits;   // workgroups that share a tile's positions
+  int32_t window, sinks;  // window 0: none
+  float scale_log2e;
+};
+
+template <class Elt, int D>
+struct PromptShape {
+  static constexpr bool kHalf = Elt::kBytes == 2;
+  static constexpr int kRowBytes = D * Elt::kBytes;
+  static constexpr int KT = kHalf ? 64 : 32;     // positions of a tile
+  static constexpr int NB = KT / 32;
+  static constexpr int NP = kRowBytes / 32;      // 16-byte pieces of a row per lane: 2 mm + h
+  static constexpr int kRowsPerWave = KT / kPromptWaves;
+  static constexpr int kLoads = kRowsPerWave * kRowBytes / 1024;  // 16-byte loads per lane of K (and of V) for a tile
+  static constexpr int kKRow = kRowBytes + 16;
+  // 16 bits: a row per dimension, 16-byte pieces of 8 positions, piece p of dimension d at p ^ (d / 8 % 8) (writes of 8 bytes then meet in
+  // no bank more often than they must); fp32: a row per position, rows 4 apart half the banks apart
+  static constexpr int kVRow = kHalf ? KT * 2 + 16 : kRowBytes + 32;
+  static constexpr int kKBytes = KT * kKRow, kVBytes = kHalf ? D * kVRow : KT * kVRow;
+};
+
+struct TileName {
+  int b, first, tokens, pos;  // sequence; first row of q, tokens, position of the first
+  int len;
+};
+
+// Tile y: sequences in order, each in tiles of `a.tokens` tokens from its last token back (the tiles with most positions start first).
+__device__ __forceinline__ TileName locate_tile(const PromptArgs& a, int y, int lane) {
+  TileName t = {-1, 0, 0, 0, 0};
+  int before = 0;
+  for (int c = 0; c < a.batch; c += 64) {
+    int begin = 0, count = 0;
+    if (c + lane < a.batch) {
+      begin = clampi(a.q_offsets[c + lane], 0, a.num_tokens);
+      count = clampi(a.q_offsets[c + lane + 1], begin, a.num_tokens) - begin;
+    }
+    const int tiles = (int)((uint32_t)(count + a.tokens - 1) / (uint32_t)a.tokens);
+    const int incl = before + wave_inclusive_scan(tiles);
+    const uint64_t past = __builtin_amdgcn_ballot_w64(incl > y);
+    if (past != 0) {
+      const int at = (int)__builtin_ctzll(past);
+      const int all = __builtin_amdgcn_readlane(count, at);
+      const int back = y - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(tiles, at));  // tile, from the last
+      const int index = __builtin_amdgcn_readlane(tiles, at) - 1 - back;
+      t.b = c + at;
+      t.len = clampi(__builtin_amdgcn_readfirstlane(a.ctx_lens[t.b]), 0, a.max_len);
+      t.first = __builtin_amdgcn_readlane(begin, at) + index * a.tokens;
+      t.tokens = min(a.tokens, all - index * a.tokens);
+      t.pos = t.len - all + index * a.tokens;
+      break;
+    }
+    before = __builtin_amdgcn_readlane(incl, 63);
+  }
+  return t;
+}
+
+// Storage type specifics of the 32x32 products.
+template <class Elt>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (std::is_same<Elt, F16>::value) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+}
+template <class Elt>
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  if constexpr (std::is_same<Elt, F16>::value) return __builtin_bit_cast(uint32_t, f16x2{(_Float16)x, (_Float16)y});
+  else return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+}
+
+template <class Elt, int D>
+__global__ __launch_bounds__(kPromptThreads)
+__attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a) {
+  using Shape = PromptShape<Elt, D>;
+  constexpr bool kHalf = Shape::kHalf;
+  constexpr int KT = Shape::KT, NB = Shape::NB, NP = Shape::NP, NL = Shape::kLoads, RW = Shape::kRowsPerWave;
+  constexpr int ROWB = Shape::kRowBytes, kKRow = Shape::kKRow, kVRow = Shape::kVRow;
+  constexpr int kLanes = ROWB / 16;               // lanes of a row in a load of K
+  constexpr int kBlocks = D / 32;
+  constexpr int kUnit = kHalf ? D / 16 : 4;       // 16 bits: dimensions of V that a lane transposes (of 4 positions)
+
+  __shared__ __attribute__((aligned(16))) unsigned char s_k[2][Shape::kKBytes];
+  __shared__ __attribute__((aligned(16))) unsigned char s_v[2][Shape::kVBytes];
+  __shared__ uint32_t s_out[2];       // 8 bits per wave: its rows of the tile lie in a page outside the pool
+  __shared__ uint32_t s_wild[2][2];   // checked pass: positions of the tile whose V row is not finite
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int h = blockIdx.x, split = blockIdx.z;
+  const int group = a.group;
+
+  const TileName t = locate_tile(a, (int)blockIdx.y, lane);
+  if (t.b < 0) return;  // (the grid holds the most tiles that any offsets give)
+  const int32_t* table = a.block_table + (size_t)t.b * a.table_pages;
+
+  // This lane's query row: token `tok` of the tile, at position `at`.
+  const int rows = t.tokens * group;
+  const int my_row = 32 * wave + col;
+  const int tok = min((int)((uint32_t)my_row / (uint32_t)group), t.tokens - 1);
+  const int at = t.pos + tok;
+  auto query_row = [&](int row) {  // row (< rows) of the tile in q and out, in rows of D
+    const uint32_t tk = (uint32_t)row / (uint32_t)group;
+    return ((size_t)t.first + tk) * (size_t)(a.kv_heads * group) + (size_t)(h * group) + (size_t)((uint32_t)row - tk * (uint32_t)group);
+  };
+  u32x4 qr[NP];
+  {
+    const char* src = (const char*)a.q + query_row(min(my_row, rows - 1)) * (size_t)ROWB + 16 * half;
+#pragma unroll
+    for (int mm = 0; mm < NP; ++mm) {
+      qr[mm] = *reinterpret_cast<const u32x4*>(src + 32 * mm);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) qr[mm][k] = Elt::scale_query(qr[mm][k], a.scale_log2e);
+    }
+  }
+  const float post = Elt::post_scale(a.scale_log2e);
+  constexpr float kShift = std::is_same<Elt, F16>::value ? 15.f : 0.f;  // weights times 2^15: fp16 then holds them down to 2^-39 of the heaviest
+
+  // Positions the tile's tokens see together: [0, sinks) and [low, high).  Cache tiles: the sinks' first, then the others.
+  const int high = t.pos + t.tokens;
+  const int low = a.window > 0 ? max(t.pos - a.window + 1, 0) : 0;
+  const int sinks = min(a.sinks, low);
+  const int sink_tiles = (sinks + KT - 1) / KT;
+  const int from = max(low / KT, sink_tiles), to = max((max(high, 0) + KT - 1) / KT, from);
+  const int all_tiles = high > 0 ? sink_tiles + to - from : 0;
+  const int per = (all_tiles + a.splits - 1) / a.splits;
+  const int first_tile = min(split * per, all_tiles), last_tile = min(first_tile + per, all_tiles);
+  auto tile_pos = [&](int i) { return (i < sink_tiles ? i : i - sink_tiles + from) * KT; };
+
+  // The wave's tokens: what decides whether it has to mask a tile, or has nothing to do with it.
+  const int wave_tok0 = (int)((uint32_t)(32 * wave) / (uint32_t)group);
+  const int wave_first = t.pos + min(wave_tok0, t.tokens - 1);
+  const int wave_last = t.pos + min((int)((uint32_t)(32 * wave + 31) / (uint32_t)group), t.tokens - 1);
+  const bool wave_works = 32 * wave < rows;
+
+  // ---- the cache's rows: global memory -> registers -> LDS -------------------------------------------------
+  u32x4 kx[NL], vx[NL];
+  uint32_t outside;
+  auto fetch = [&](int p0) {
+    const int p = p0 + wave * RW;  // the wave's rows of the tile lie in one page
+    const int entry = p >> a.page_shift, in_page = p & ((1 << a.page_shift) - 1);
+    const int page = entry < a.table_pages ? __builtin_amdgcn_readfirstlane(table[entry]) : -1;
+    const bool good = (uint32_t)page < (uint32_t)a.num_pages;
+    outside = !good && p < high ? 1u : 0u;
+    const int there = good ? clampi(t.len - (entry << a.page_shift), 0, 1 << a.page_shift) : 0;  // rows of the page that are the sequence's
+    const size_t slab = (((size_t)(good ? page : 0) * (size_t)a.kv_heads + (size_t)h) << a.page_shift) * (size_t)ROWB;
+    const __amdgpu_buffer_rsrc_t kp = slab_resource((const char*)a.k + slab, (uint32_t)(there * ROWB));
+    const __amdgpu_buffer_rsrc_t vp = slab_resource((const char*)a.v + slab, (uint32_t)(there * ROWB));
+    const uint32_t base = (uint32_t)in_page * ROWB;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) kx[i] = __builtin_amdgcn_raw_buffer_load_b128(kp, base + 16u * (uint32_t)lane + 1024u * i, 0, 0);
+    if constexpr (kHalf) {
+      // lane: positions 4 (lane / 16) + i of the wave's 16, dimensions kUnit (lane % 16) on
+      const uint32_t vat = base + (uint32_t)(4 * (lane >> 4)) * ROWB + (uint32_t)(lane & 15) * (kUnit * 2);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (kUnit == 8) vx[i] = __builtin_amdgcn_raw_buffer_load_b128(vp, vat + (uint32_t)i * ROWB, 0, 0);
+        else {
+          const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(vp, vat + (uint32_t)i * ROWB, 0, 0);
+          vx[i / 2][2 * (i & 1)] = w[0];
+          vx[i / 2][2 * (i & 1) + 1] = w[1];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) vx[i] = __builtin_amdgcn_raw_buffer_load_b128(vp, base + 16u * (uint32_t)lane + 1024u * i, 0, 0);
+    }
+  };
+  auto lay_down = [&](int buf, auto checked) {
+    constexpr bool kChecked = decltype(checked)::value;
+    if (lane == 0) reinterpret_cast<unsigned char*>(&s_out[buf])[wave] = (unsigned char)outside;
+    unsigned char* kd = &s_k[buf][(wave * RW + lane / kLanes) * kKRow + 16 * (lane % kLanes)];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) *reinterpret_cast<u32x4*>(kd + i * (64 / kLanes) * kKRow) = kx[i];
+    if constexpr (kHalf) {
+      constexpr int W = kUnit / 2;  // dwords of a position
+      uint32_t x[4][W];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int k = 0; k < W; ++k) x[i][k] = kUnit == 8 ? vx[i][k] : vx[i / 2][2 * (i & 1) + k];
+      }
+      const int quad = lane >> 4;  // positions 16 wave + 4 quad ..
+      if constexpr (kChecked) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bool wild = false;
+#pragma unroll
+          for (int k = 0; k < W; ++k) {
+            const uint32_t w = x[i][k];
+            const bool lo = Elt::not_finite(w & 0xffffu), hi = Elt::not_finite(w & 0xffff0000u);
+            wild = wild || lo || hi;
+            x[i][k] = (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
+          }
+          if (wild) atomicOr(&s_wild[buf][wave / 2], 1u << (16 * (wave & 1) + 4 * quad + i));
+        }
+      }
+      // piece of 8 positions: 0-3 and 8-11 of the wave's 16 (quads 0, 2), or 4-7 and 12-15 (quads 1, 3)
+      const int piece = 2 * wave + (quad & 1), within = 8 * (quad >> 1);
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        const int d = kUnit * (lane & 15) + j;
+        const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
+        const u32x2 w = {__builtin_amdgcn_perm(x[1][j / 2], x[0][j / 2], sel), __builtin_amdgcn_perm(x[3][j / 2], x[2][j / 2], sel)};
+        *reinterpret_cast<u32x2*>(&s_v[buf][d * kVRow + 16 * (piece ^ ((d >> 3) & 7)) + within]) = w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = wave * RW + i * (64 / kLanes) + lane / kLanes;
+        u32x4 w = vx[i];
+        if constexpr (kChecked) {
+          bool wild = false;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            wild = wild || Elt::not_finite(w[k]);
+            w[k] = Elt::not_finite(w[k]) ? 0u : w[k];
+          }
+          if (wild) atomicOr(&s_wild[buf][0], 1u << row);
+        }
+        *reinterpret_cast<u32x4*>(&s_v[buf][row * kVRow + 16 * (lane % kLanes)]) = w;
+      }
+    }
+  };
+
+  float ref = -INFINITY, lsum = 0.f;  // reference of the weights: the largest unscaled score; this lane's share of their sum
+  f32x16 O[kBlocks];
+  auto sees = [&](int p) { return p <= at && (a.window == 0 || p > at - a.window || p < a.sinks); };
+
+  auto compute = [&](int buf, int p0, auto checked) {
+    constexpr bool kChecked = decltype(checked)::value;
+    if (!wave_works || p0 > wave_last) return;
+    if (a.window > 0 && p0 + KT - 1 <= wave_first - a.window && p0 >= a.sinks) return;
+    f32x16 S[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) S[n][r] = 0.f;
+      const unsigned char* kr = &s_k[buf][(32 * n + col) * kKRow + 16 * half];
+#pragma unroll
+      for (int mm = 0; mm < NP; ++mm) {
+        const u32x4 km = *reinterpret_cast<const u32x4*>(kr + 32 * mm);
+        if constexpr (kHalf) {
+          S[n] = mfma32<Elt>(km, qr[mm], S[n]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t kw = km[k], qw = qr[mm][k];
+            S[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, kw), __builtin_bit_cast(float, qw), S[n], 0, 0, 0);
+          }
+        }
+      }
+    }
+    const uint32_t out_bits = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[buf]);
+    const bool whole = p0 + KT - 1 <= wave_first && (a.window == 0 || p0 > wave_last - a.window || p0 + KT <= a.sinks) && out_bits == 0;
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int i = 32 * n + 8 * (r / 4) + r % 4;  // (+ 4 half)
+          const bool ok = sees(p0 + i + 4 * half) && (out_bits >> (8 * (i / RW)) & 1u) == 0;
+          S[n][r] = ok ? S[n][r] : -INFINITY;
+        }
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S[n][r]);
+    }
+    if (__builtin_amdgcn_ballot_w64(mx > ref) != 0) {
+      const Swapped sw = swap_lanes<32>(mx, mx);
+      const float ref_new = fmaxf(ref, fmaxf(sw.first, sw.second)), safe = ref_new == -INFINITY ? 0.f : ref_new;
+      const float alpha = __builtin_amdgcn_exp2f((ref - safe) * post);
+      ref = ref_new;
+      lsum *= alpha;
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) O[e] *= alpha;
+    }
+    const float safe = ref == -INFINITY ? 0.f : ref;
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        S[n][r] = __builtin_amdgcn_exp2f(fmaf(S[n][r] - safe, post, kShift));
+        sum[r & 3] += S[n][r];
+      }
+      lsum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    }
+    if constexpr (kHalf) {
+      u32x4 P[NB][2];
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) P[n][c][k] = pack2<Elt>(S[n][8 * c + 2 * k], S[n][8 * c + 2 * k + 1]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) {
+        const int d = 32 * e + col;
+        const unsigned char* vr = &s_v[buf][d * kVRow];
+        const int turn = (d >> 3) & 7;
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const u32x4 vm = *reinterpret_cast<const u32x4*>(vr + 16 * ((4 * n + 2 * c + half) ^ turn));
+            O[e] = mfma32<Elt>(vm, P[n][c], O[e]);
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float vm = *reinterpret_cast<const float*>(&s_v[buf][(8 * (r / 4) + r % 4 + 4 * half) * kVRow + 4 * (32 * e + col)]);
+          O[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vm, S[0][r], O[e], 0, 0, 0);
+        }
+      }
+    }
+    if constexpr (kChecked) {
+      // Values of V that are not finite were left out of the products; here they meet the weights of the queries that see them, and of no others
+      // (0 * Inf would be NaN).
+#pragma unroll 1
+      for (int w = 0; w < NB; ++w) {
+#pragma unroll 1
+        for (uint32_t todo = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_wild[buf][w]); todo != 0; todo &= todo - 1) {
+          const int i = __builtin_ctz(todo);           // position 32 w + i: scores' register 4 (i / 8) + i % 4 of half i / 4 % 2
+          const int p = p0 + 32 * w + i, r_of = 4 * (i >> 3) + (i & 3);
+          float x = 0.f;
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x = n == w && r == r_of ? S[n][r] : x;
+          }
+          x = __shfl(x, 32 * ((i >> 2) & 1) + col, 64);
+          const int row = pool_row(table, p, a.page_shift, a.num_pages);
+          if (row < 0 || !sees(p)) continue;
+          const size_t page = (size_t)(row >> a.page_shift), in_page = (size_t)(row & ((1 << a.page_shift) - 1));
+          const char* src = (const char*)a.v + (((page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) + in_page) * (size_t)ROWB;
+#pragma unroll
+          for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+              float vf[4];
+              const char* from4 = src + (32 * e + 8 * g + 4 * half) * Elt::kBytes;
+              if constexpr (kHalf) Elt::unpack4(*reinterpret_cast<const u32x2*>(from4), vf);
+              else Elt::unpack4(*reinterpret_cast<const u32x4*>(from4), vf);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const bool wild = !(fabsf(vf[k]) < INFINITY);
+                O[e][4 * g + k] = wild ? fmaf(x, vf[k], O[e][4 * g + k]) : O[e][4 * g + k];
+              }
+            }
+          }
+        }
+      }
+    }
+  };
+
+  auto walk = [&](auto checked) {
+    constexpr bool kChecked = decltype(checked)::value;
+    ref = -INFINITY;
+    lsum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[e][r] = 0.f;
+    }
+    if (first_tile >= last_tile) return;
+    if (kChecked) {
+      if (tid < 4) s_wild[tid >> 1][tid & 1] = 0u;
+      __syncthreads();
+    }
+    fetch(tile_pos(first_tile));
+    lay_down(0, checked);
+    __syncthreads();
+    int buf = 0;
+    for (int i = first_tile; i < last_tile; ++i) {
+      if (i + 1 < last_tile) fetch(tile_pos(i + 1));
+      compute(buf, tile_pos(i), checked);
+      if (kChecked) {
+        __syncthreads();
+        if (tid < 2) s_wild[buf][tid] = 0u;  // (for the tile after next)
+      }
+      if (i + 1 < last_tile) lay_down(buf ^ 1, checked);
+      __syncthreads();
+      buf ^= 1;
+    }
+  };
+  walk(std::false_type{});
+  {
+    float z = 0.f;  // stays 0 unless some output is Inf or NaN
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z = fmaf(O[e][r], 0.f, z);
+    }
+    if (__builtin_expect(__syncthreads_or(z != 0.f), 0)) walk(std::true_type{});
+  }
+
+  const Swapped both = swap_lanes<32>(lsum, lsum);
+  lsum = both.first + both.second;
+  if (a.splits > 1) {
+    if (my_row < rows) {
+      const size_t slot = ((size_t)blockIdx.y * a.kv_heads + h) * (size_t)a.splits + (size_t)split;
+      const size_t row = slot * kPromptRows + (size_t)my_row;
+      if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * row) = f32x2{ref, lsum};
+      float* acc = a.part_acc + row * D + 4 * half;
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4*>(acc + 32 * e + 8 * g) = f32x4{O[e][4 * g], O[e][4 * g + 1], O[e][4 * g + 2], O[e][4 * g + 3]};
+      }
+    }
+    return;
+  }
+  // The wave's rows through LDS, so that they are stored whole (its own part of the first half, which nobody reads any more).
+  const float sum = lsum != 0.f ? lsum : 1.f;
+  static_assert(32 * kPromptWaves * kKRow <= 2 * Shape::kKBytes || kHalf == false, "the tile's outputs fit");
+  if constexpr (kHalf) {
+    unsigned char* mine = &s_k[0][0] + wave * 32 * kKRow;
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const u32x2 w = {pack2<Elt>(O[e][4 * g] / sum, O[e][4 * g + 1] / sum), pack2<Elt>(O[e][4 * g + 2] / sum, O[e][4 * g + 3] / sum)};
+        *reinterpret_cast<u32x2*>(mine + col * kKRow + 2 * (32 * e + 8 * g + 4 * half)) = w;
+      }
+    }
+    wave_lds_order();
+#pragma unroll
+    for (int i = 0; i < 32 * kLanes / 64; ++i) {
+      const int r = i * (64 / kLanes) + lane / kLanes;
+      if (32 * wave + r < rows)
+        *reinterpret_cast<u32x4*>((char*)a.out + query_row(32 * wave + r) * (size_t)ROWB + 16 * (lane % kLanes)) =
+            *reinterpret_cast<const u32x4*>(mine + r * kKRow + 16 * (lane % kLanes));
+    }
+  } else if (my_row < rows) {
+    float* out = (float*)a.out + query_row(my_row) * (size_t)D + 4 * half;
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(out + 32 * e + 8 * g) = f32x4{O[e][4 * g] / sum, O[e][4 * g + 1] / sum, O[e][4 * g + 2] / sum, O[e][4 * g + 3] / sum};
+    }
+  }
+}
+
+// The states of the workgroups that shared a tile's positions become one: a thread has four columns of a row.
+template <class Elt, int D>
+__global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a) {
+  const int lane = threadIdx.x & 63, h = blockIdx.x;
+  const TileName t = locate_tile(a, (int)blockIdx.y, lane);
+  if (t.b < 0) return;
+  const float post = Elt::post_scale(a.scale_log2e);
+  const int row = (int)(blockIdx.z * 256 + threadIdx.x) / (D / 4), column = (int)threadIdx.x % (D / 4) * 4;
+  if (row >= t.tokens * a.group) return;
+  const size_t slot0 = ((size_t)blockIdx.y * a.kv_heads + h) * (size_t)a.splits;
+  float M = -INFINITY, L = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; ++s) {
+    const size_t at = (slot0 + (size_t)s) * kPromptRows + (size_t)row;
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * at);
+    const f32x4 os = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + column);
+    if (ml[1] == 0.f) continue;  // (nothing seen there; a NaN sum counts)
+    const float before = M;
+    M = fmaxf(M, ml[0]);
+    const float safe = M == -INFINITY ? 0.f : M;
+    const float old = __builtin_amdgcn_exp2f((before - safe) * post), w = __builtin_amdgcn_exp2f((ml[0] - safe) * post);
+    L = fmaf(L, old, w * ml[1]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) o[k] = fmaf(o[k], old, w * os[k]);
+  }
+  const float sum = L != 0.f ? L : 1.f;
+  const uint32_t tk = (uint32_t)row / (uint32_t)a.group;
+  const size_t to = (((size_t)t.first + tk) * (size_t)(a.kv_heads * a.group) + (size_t)(h * a.group) + (size_t)((uint32_t)row - tk * (uint32_t)a.group)) * D + column;
+  if constexpr (Elt::kBytes == 2) {
+    *reinterpret_cast<u32x2*>((char*)a.out + to * 2) = u32x2{pack2<Elt>(o[0] / sum, o[1] / sum), pack2<Elt>(o[2] / sum, o[3] / sum)};
+  } else {
+    *reinterpret_cast<f32x4*>((float*)a.out + to) = f32x4{o[0] / sum, o[1] / sum, o[2] / sum, o[3] / sum};
+  }
+}
+
+template <class Elt, int D>
+int run_prompt(const PromptArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((prompt_kernel<Elt, D>), dim3((unsigned)a.kv_heads, (unsigned)a.tiles, (unsigned)a.splits), dim3(kPromptThreads), 0, stream, a);
+  const int rc = launched();
+  if (rc != SPAN_OK || a.splits == 1) return rc;
+  const unsigned z = (unsigned)(kPromptRows * (D / 4) / 256);
+  hipLaunchKernelGGL((prompt_merge_kernel<Elt, D>), dim3((unsigned)a.kv_heads, (unsigned)a.tiles, z), dim3(256), 0, stream, a);
+  return launched();
+}
+
+}  // namespace
+}  // namespace spanattn
+
+extern "C" int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                                 const int32_t* ctx_lens, const int32_t* q_offsets, float scale, void* out) {
+  using namespace spanattn;
+  const int rc = check_paged(desc);
+  if (rc != SPAN_OK) return rc;
+  if (!block_table || !ctx_lens || !q_offsets || !k_pages || !v_pages) return SPAN_ERR_NULL;
+  if (desc->num_tokens == 0) return SPAN_OK;
+  if (!q || !out) return SPAN_ERR_NULL;
+  const PromptPlan p = plan_prompt(desc);
+  if (p.tiles > 65535) return SPAN_ERR_SHAPE;
+  const size_t need = prompt_workspace(desc, p);
+  if (need > 0 && (!desc->workspace || ((uintptr_t)desc->workspace & 255u) || desc->workspace_bytes < need)) return SPAN_ERR_WORKSPACE;
+  PromptArgs a;
+  a.q = q;
+  a.k = k_pages;
+  a.v = v_pages;
+  a.out = out;
+  a.block_table = block_table;
+  a.ctx_lens = ctx_lens;
+  a.q_offsets = q_offsets;
+  a.part_ml = need ? (float*)desc->workspace : nullptr;
+  a.part_acc = need ? (float*)((char*)desc->workspace + p.acc) : nullptr;
+  a.batch = desc->batch;
+  a.kv_heads = desc->kv_heads;
+  a.group = desc->heads / desc->kv_heads;
+  a.table_pages = desc->table_pages;
+  a.page_shift = page_shift(desc);
+  a.num_pages = desc->num_pages;
+  a.num_tokens = desc->num_tokens;
+  a.max_len = capacity(desc);
+  a.tokens = p.tokens;
+  a.tiles = p.tiles;
+  a.splits = p.splits;
+  a.window = desc->window < a.max_len ? desc->window : 0;  // (a window of the whole table hides nothing)
+  a.sinks = desc->sinks < a.max_len ? desc->sinks : a.max_len;
+  a.scale_log2e = scale * 1.4426950408889634f;
+  hipStream_t stream = (hipStream_t)desc->stream;
+  const bool d128 = desc->head_dim == 128;
+  switch (desc->dtype) {
+    case SPAN_F32: return d128 ? run_prompt<F32, 128>(a, stream) : run_prompt<F32, 64>(a, stream);
+    case SPAN_F16: return d128 ? run_prompt<F16, 128>(a, stream) : run_prompt<F16, 64>(a, stream);
+    default: return d128 ? run_prompt<BF16, 128>(a, stream) : run_prompt<BF16, 64>(a, stream);
+  }
+}

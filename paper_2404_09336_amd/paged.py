@@ -29,7 +29,7 @@ def _library():
     if not _signed:
         P, F, DP = ctypes.c_void_p, ctypes.c_float, ctypes.POINTER(_PagedDesc)
         for name, args in (("paged_append", [P] * 9), ("paged_decode_attn", [P] * 5 + [F, P, P]), ("paged_span_decode_attn", [P] * 7 + [F, P, P]),
-                           ("paged_evict", [P] * 9), ("paged_workspace_init", []), ("paged_check", [])):
+                           ("paged_prompt_attn", [P] * 6 + [F, P]), ("paged_evict", [P] * 9), ("paged_workspace_init", []), ("paged_check", [])):
             fn = getattr(lib, name)
             fn.argtypes, fn.restype = [DP] + args, ctypes.c_int
         lib.paged_workspace_bytes.argtypes, lib.paged_workspace_bytes.restype = [DP, ctypes.c_int], ctypes.c_size_t
@@ -203,6 +203,34 @@ def prepare_paged_span_decode_attn(q, k_pages, v_pages, block_table, span_offset
 def paged_span_decode_attn(q, k_pages, v_pages, block_table, span_offsets, span_starts, span_ends, scale, out=None, **kw):
     """span_decode_attn over a cache in pages.  Returns `out`."""
     return prepare_paged_span_decode_attn(q, k_pages, v_pages, block_table, span_offsets, span_starts, span_ends, scale, out, **kw)()
+
+
+def prepare_paged_prompt_attn(q, k_pages, v_pages, block_table, ctx_lens, q_offsets, scale, out=None, *, window=0, sinks=0, workspace=None,
+                              stream=None) -> PreparedCall:
+    """q [num_tokens, heads, head_dim], q_offsets int32 GPU tensor [batch + 1], out shaped and typed like q."""
+    import torch
+    lib = _library()
+    B, KV, P, D, N, TP, device = _cache(k_pages, v_pages, block_table, ctx_lens)
+    if q.dim() != 3:
+        raise ValueError("expected q [num_tokens, heads, head_dim]")
+    T, H = q.shape[:2]
+    _on_gpu(q, "q", k_pages.dtype, (T, H, D), device)
+    _on_gpu(q_offsets, "q_offsets", torch.int32, (B + 1,), device)
+    if out is None:
+        out = torch.empty_like(q)
+    _on_gpu(out, "out", q.dtype, (T, H, D), device)
+    desc = make_paged_desc(B, H, KV, D, _dtype_code(k_pages), P, N, TP, num_tokens=T, window=window, sinks=sinks, stream=_stream(stream, device))
+    _check(desc, "paged_prompt_attn")
+    workspace = _take_workspace(desc, PAGED_PROMPT, workspace, device, False)
+    args = (ctypes.byref(desc), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), ctx_lens.data_ptr(), q_offsets.data_ptr(),
+            float(scale), out.data_ptr())
+    keep = (q, k_pages, v_pages, block_table, ctx_lens, q_offsets, workspace)
+    return PreparedCall("paged_prompt_attn", lib.paged_prompt_attn, desc, args, out, keep)
+
+
+def paged_prompt_attn(q, k_pages, v_pages, block_table, ctx_lens, q_offsets, scale, out=None, **kw):
+    """Causal attention of the new tokens of every sequence over its cache, optionally with a window and sinks.  Returns `out`."""
+    return prepare_paged_prompt_attn(q, k_pages, v_pages, block_table, ctx_lens, q_offsets, scale, out, **kw)()
 
 
 def prepare_paged_evict(k_pages, v_pages, block_table, ctx_lens, weights, budget, *, sinks=0, recent=0, positions=None, weights_out=None,

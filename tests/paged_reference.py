@@ -37,7 +37,7 @@ class Pages:
     def rows(self, pool, b, positions):
         """[kv_heads, len(positions), head_dim] in 64 bits."""
         p = torch.as_tensor(np.asarray(positions, dtype=np.int64))
-        page = self.table[b, p // self.page].long()
+        page = self.table[b, p // self.page].long().clamp(0, pool.shape[0] - 1)  # (who names others masks what is there)
         return pool[page, :, p % self.page].transpose(0, 1).double()
 
 

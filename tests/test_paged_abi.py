@@ -33,7 +33,8 @@ def call(name, d, *args):
 def test_library_exports_every_declared_symbol():
     text = open(os.path.join(ROOT, "include", "span_paged.h")).read()
     names = set(re.findall(r"\b(paged_\w+)\s*\(", re.sub(r"/\*.*?\*/", "", text, flags=re.S)))
-    assert {"paged_append", "paged_decode_attn", "paged_span_decode_attn", "paged_evict", "paged_workspace_bytes", "paged_workspace_init", "paged_check"} <= names
+    assert {"paged_append", "paged_decode_attn", "paged_span_decode_attn", "paged_prompt_attn", "paged_evict", "paged_workspace_bytes",
+            "paged_workspace_init", "paged_check"} <= names
     for name in names:
         assert hasattr(paged._library(), name), name
 
@@ -51,6 +52,7 @@ def test_shapes_are_refused(bad):
     assert call("paged_append", d, *[FAR] * 9) == -2
     assert call("paged_decode_attn", d, *[FAR] * 5, 1.0, None, FAR) == -2
     assert call("paged_span_decode_attn", d, *[FAR] * 7, 1.0, None, FAR) == -2
+    assert call("paged_prompt_attn", d, *[FAR] * 6, 1.0, FAR) == -2
     assert call("paged_evict", d, *[FAR] * 9) == -2
     assert call("paged_workspace_init", d) == -2
 
@@ -72,6 +74,10 @@ def test_missing_pointers_are_refused():
     d = with_workspace(paged.PAGED_SPAN_DECODE, num_intervals=3)
     for i in range(7):
         assert call("paged_span_decode_attn", d, *without(7, i), 1.0, None, FAR) == -1
+    d = with_workspace(paged.PAGED_PROMPT, num_tokens=20)
+    for i in range(6):
+        assert call("paged_prompt_attn", d, *without(6, i), 1.0, FAR) == -1
+    assert call("paged_prompt_attn", d, *[FAR] * 6, 1.0, None) == -1
     for i in range(6):
         assert call("paged_append", desc(num_tokens=2), *without(6, i), FAR, FAR, FAR) == -1
     d = with_workspace(paged.PAGED_EVICT, budget=8)
@@ -95,15 +101,12 @@ def test_budgets_are_refused():
 @pytest.mark.parametrize("use", range(6))
 def test_workspaces_are_refused(use):
     """Missing, a byte short, misaligned."""
-    d = desc(budget=20, table_pages=64, num_pages=200, num_intervals=4)
+    d = desc(budget=20, table_pages=64, num_pages=200, num_intervals=4, num_tokens=100)
     need = paged.paged_workspace_bytes(d, use)
-    assert need % 256 == 0
-    if use == paged.PAGED_PROMPT:
-        return
-    assert need > 0
+    assert need > 0 and need % 256 == 0
     run = {0: lambda: call("paged_decode_attn", d, *[FAR] * 5, 1.0, None, FAR), 1: lambda: call("paged_decode_attn", d, *[FAR] * 5, 1.0, FAR, FAR),
            2: lambda: call("paged_span_decode_attn", d, *[FAR] * 7, 1.0, None, FAR), 3: lambda: call("paged_span_decode_attn", d, *[FAR] * 7, 1.0, FAR, FAR),
-           5: lambda: call("paged_evict", d, *[FAR] * 9)}[use]
+           4: lambda: call("paged_prompt_attn", d, *[FAR] * 6, 1.0, FAR), 5: lambda: call("paged_evict", d, *[FAR] * 9)}[use]
     for at, size in ((None, need), (FAR, need - 1), (FAR + 64, need)):
         d.workspace, d.workspace_bytes = at, size
         assert run() == -4
@@ -115,6 +118,11 @@ def test_workspace_init_needs_the_counters():
     for at, size in ((None, 1 << 20), (FAR, 100 * 16 * 4 - 1), (FAR + 16, 1 << 20)):
         d.workspace, d.workspace_bytes = at, size
         assert call("paged_workspace_init", d) == -4
+
+
+def test_prompts_without_tokens_and_with_too_many():
+    assert call("paged_prompt_attn", desc(num_tokens=0), None, *[FAR] * 5, 1.0, None) == 0
+    assert call("paged_prompt_attn", desc(num_tokens=65536 * 32), *[FAR] * 6, 1.0, FAR) == -2  # tiles of 32 tokens of 4 heads: the grid's limit
 
 
 def slices(lens, room):
