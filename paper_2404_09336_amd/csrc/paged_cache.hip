@@ -94,23 +94,25 @@ struct EvictArgs {
   float* weights_out;
   int32_t* positions_out;
   int32_t* new_lens;
-  int32_t* moves;  // per (sequence, KV head): count, `most` slots to move to, `most` to move from
+  int32_t* moves;  // per (sequence, KV head): count, 0, `most` pairs of slots, to and from
   int32_t kv_heads, table_pages, page_shift, num_pages, max_len, budget, sinks, recent, most;
 };
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kHoleList = 4096;  // free slots whose list fits LDS
 
-// Which rows stay, one workgroup per (sequence, KV head).  Every slot has a 32-bit key that orders as it is to be kept: largest for the protected ones, then the weight's
-// bits made monotone; equal keys by slot.  The budget-th largest key is found two bits at a time, counting with ballots the keys that reach the three candidates of
-// a step (a histogram's atomics would meet in few bins: weights share their exponents); then the waves, each with its own run of slots, count
-// equal keys, free slots and rows to move, and write the lists in order.  Keys of up to kKeys slots stay in LDS, those of longer caches are made
-// again from the weights each time.
+// Which rows stay, one workgroup per (sequence, KV head).  Every slot has a 32-bit key that orders as it is to be kept: largest for the protected ones, then the
+// weight's bits made monotone; equal keys by slot.  The budget-th largest key is found digit by digit (11, 11 and 10 bits) with histograms in LDS; the
+// first digit holds a weight's exponent and two bits of its mantissa, so that even weights of one size spread over some bins, and the protected ones, which
+// all meet, are counted apart.  Then the waves, each with its own run of slots, count equal keys, free slots and rows to move in order.
+// kKeys: slots of a thread, whose keys stay in registers; 0: any number, keys made again from the weights each time.  us, 16 x 8 caches of ~4350 slots
+// and 5 x 16 of ~6500, with keys in LDS and two bits a step by ballots (16 rounds) -> so: 30.5 and 62.9 -> 12.6 and 19.8.
 template <int kKeys>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs a) {
-  __shared__ uint32_t s_key[kKeys];
-  __shared__ int s_sum[3][4];
-  __shared__ int s_wave[3][kSelectWaves];
-  __shared__ int s_last[kSelectWaves];
+  __shared__ int s_bins[2048];
+  __shared__ int s_holes[kHoleList];
+  __shared__ int s_wave[4][kSelectWaves];
+  __shared__ int s_pick[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x, b = bh / a.kv_heads;
   const int n = clampi(a.ctx_lens[b], 0, a.max_len), keep = a.budget;
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
   const int32_t* positions = a.positions != nullptr ? a.positions + row : nullptr;
   float* weights_out = a.weights_out + row;
   int32_t* positions_out = a.positions_out != nullptr ? a.positions_out + row : nullptr;
-  int32_t* moves = a.moves + (size_t)bh * (size_t)(1 + 2 * a.most);
+  int32_t* moves = a.moves + (size_t)bh * (size_t)(2 + 2 * a.most);
   if (n <= keep) {
     if (tid == 0) moves[0] = 0;
     for (int i = tid; i < n; i += kSelectThreads) {
@@ -128,122 +130,208 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
     }
     return;
   }
-  // the largest position held
+  // the wave's run of slots, in pieces of 64
+  const int run = ((n + 63) / 64 + kSelectWaves - 1) / kSelectWaves * 64;
+  const int begin = min(wave * run, n), end = min(begin + run, n);
+  auto pieces = [&](auto&& f) {
+    if constexpr (kKeys > 0) {
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) {
+        if (begin + 64 * j < end) f(j, begin + 64 * j + lane);
+      }
+    } else {
+      for (int i0 = begin; i0 < end; i0 += 64) f(0, i0 + lane);
+    }
+  };
+  constexpr int kHeld = kKeys > 0 ? kKeys : 1;
+  constexpr bool kRemember = kKeys > 0 && kKeys <= 16;  // weights and positions too (32 of each would spill)
+  uint32_t held[kHeld];  // keys
+  float weight[kHeld];
+  // the weights, and the largest position held
   int last = n - 1;
+  if constexpr (kKeys > 0) {
+#pragma unroll
+    for (int j = 0; j < kKeys; ++j) weight[j] = begin + 64 * j < end ? weights[min(begin + 64 * j + lane, n - 1)] : 0.f;
+  }
+  int position[kHeld];
   if (positions != nullptr) {
     last = 0;
-    for (int i = tid; i < n; i += kSelectThreads) last = max(last, positions[i]);
-    last = __builtin_amdgcn_readlane(wave_inclusive_max(last), 63);
-    if (lane == 0) s_last[wave] = last;
-    __syncthreads();
-    last = 0;
+    if constexpr (kKeys > 0) {
 #pragma unroll
-    for (int w = 0; w < kSelectWaves; ++w) last = max(last, s_last[w]);
+      for (int j = 0; j < kKeys; ++j) position[j] = begin + 64 * j < end ? positions[min(begin + 64 * j + lane, n - 1)] : 0;
+#pragma unroll
+      for (int j = 0; j < kKeys; ++j) last = max(last, position[j]);
+    } else {
+      for (int i = tid; i < n; i += kSelectThreads) last = max(last, positions[i]);
+    }
+    last = __builtin_amdgcn_readlane(wave_inclusive_max(last), 63);
+    if (lane == 0) s_wave[3][wave] = last;
   }
-  auto make_key = [&](int i) -> uint32_t {
-    const int p = positions != nullptr ? positions[i] : i;
+  s_bins[tid] = s_bins[tid + kSelectThreads] = 0;
+  __syncthreads();
+  auto over_waves = [&](int which) { return lane < kSelectWaves ? s_wave[which][lane] : 0; };  // (summed or scanned by every wave for itself)
+  if (positions != nullptr) last = __builtin_amdgcn_readlane(wave_inclusive_max(over_waves(3)), 63);
+  auto key_of = [&](int p, uint32_t u) -> uint32_t {
     if (p < a.sinks || last - p < a.recent) return 0xffffffffu;
-    const uint32_t u = __builtin_bit_cast(uint32_t, weights[i]);
     if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;  // NaN
     if (u == 0x80000000u) return 0x80000000u;        // -0 is 0
     return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
   };
-  const bool held = n <= kKeys;
-  if (held) {
-    for (int i = tid; i < n; i += kSelectThreads) s_key[i] = make_key(i);
-  }
-  if (tid < 12) s_sum[tid / 4][tid % 4] = 0;
-  __syncthreads();
-  auto key = [&](int i) -> uint32_t { return held ? s_key[i] : make_key(i); };
-
-  uint32_t at = 0;  // the largest key that `keep` keys reach, as far as it is known
-  int round = 0;
-  for (int shift = 30; shift >= 0; shift -= 2, round = round == 2 ? 0 : round + 1) {
-    int reach[3] = {0, 0, 0};
-    for (int i0 = wave * 64; i0 < n; i0 += kSelectThreads) {
-      const int i = i0 + lane;
-      const uint32_t x = i < n ? key(i) : 0u;
+  if constexpr (kKeys > 0) {
 #pragma unroll
-      for (int k = 0; k < 3; ++k) reach[k] += __popcll(__builtin_amdgcn_ballot_w64(i < n && x >= at + ((uint32_t)(k + 1) << shift)));
-    }
-    const int next = round == 2 ? 0 : round + 1;
-    if (tid < 4) s_sum[next][tid] = 0;  // (last read two barriers ago)
-    if (lane < 3) atomicAdd(&s_sum[round][lane], lane == 0 ? reach[0] : (lane == 1 ? reach[1] : reach[2]));
-    __syncthreads();
-    const int c1 = s_sum[round][0], c2 = s_sum[round][1], c3 = s_sum[round][2];
-    at += (uint32_t)(c3 >= keep ? 3 : (c2 >= keep ? 2 : (c1 >= keep ? 1 : 0))) << shift;
+    for (int j = 0; j < kKeys; ++j) held[j] = key_of(positions != nullptr ? position[j] : begin + 64 * j + lane, __builtin_bit_cast(uint32_t, weight[j]));
   }
-
-  // waves' runs of slots
-  const int run = ((n + 63) / 64 + kSelectWaves - 1) / kSelectWaves * 64;
-  const int begin = min(wave * run, n), end = min(begin + run, n);
+  auto key = [&](int j, int i) -> uint32_t {
+    if constexpr (kKeys > 0) return held[j];
+    else return i < n ? key_of(positions != nullptr ? positions[i] : i, __builtin_bit_cast(uint32_t, weights[i])) : 0u;
+  };
+  auto count_if = [&](bool x) { return (int)__popcll(__builtin_amdgcn_ballot_w64(x)); };
   auto lanes_below = [&](uint64_t who) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u)); };
-  int above = 0, equal = 0;
-  for (int i0 = begin; i0 < end; i0 += 64) {
-    const int i = i0 + lane;
-    const uint32_t x = i < end ? key(i) : 0u;
-    above += __popcll(__builtin_amdgcn_ballot_w64(i < end && x > at));
-    equal += __popcll(__builtin_amdgcn_ballot_w64(i < end && x == at));
-  }
-  if (lane == 0) {
-    s_wave[0][wave] = above;
-    s_wave[1][wave] = equal;
-  }
+
+  int safe = 0;
+  pieces([&](int j, int i) {
+    const uint32_t x = key(j, i);
+    safe += count_if(i < end && x == 0xffffffffu);
+    if (i < end && x != 0xffffffffu) atomicAdd(&s_bins[2047 - (x >> 21)], 1);
+  });
+  if (lane == 0) s_wave[0][wave] = safe;
   __syncthreads();
-  int ties = keep, ties_before = 0;  // of the slots with key `at` so many stay: the first
-  for (int w = 0; w < kSelectWaves; ++w) {
-    ties -= s_wave[0][w];
-    ties_before += w < wave ? s_wave[1][w] : 0;
-  }
-  __syncthreads();
-  // pass 0 counts the wave's free slots below the budget and the rows it has to move, pass 1 writes them down
-  int free_before = 0, move_before = 0, count = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    int tied = ties_before, holes = free_before, movers = move_before;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-      const int i = i0 + lane;
-      const bool in = i < end;
-      const uint32_t x = in ? key(i) : 0u;
-      const uint64_t eq = __builtin_amdgcn_ballot_w64(in && x == at);
-      const bool stays = in && (x > at || (x == at && tied + lanes_below(eq) < ties));
-      tied += __popcll(eq);
-      const bool hole = in && !stays && i < keep, mover = stays && i >= keep;
-      const uint64_t hole_lanes = __builtin_amdgcn_ballot_w64(hole), mover_lanes = __builtin_amdgcn_ballot_w64(mover);
-      if (pass == 1) {
-        if (hole) moves[1 + holes + lanes_below(hole_lanes)] = i;
-        if (mover) moves[1 + a.most + movers + lanes_below(mover_lanes)] = i;
-        if (stays && i < keep) {
-          weights_out[i] = weights[i];
-          if (positions_out != nullptr) positions_out[i] = positions[i];
-        }
+  safe = __builtin_amdgcn_readlane(wave_inclusive_scan(over_waves(0)), 63);
+  uint32_t at = 0xffffffffu;  // the key of the last row that stays
+  int ties = keep;            // of the slots with that key so many stay, the first
+  if (safe < keep) {
+    ties = keep - safe;
+    at = 0;
+#pragma unroll
+    for (int digit = 0; digit < 3; ++digit) {  // (bins count from the largest)
+      const int shift = digit == 0 ? 21 : (digit == 1 ? 10 : 0);
+      if (digit > 0) {
+        const int above = digit == 1 ? 21 : 10, mask = digit == 1 ? 2047 : 1023;
+        pieces([&](int j, int i) {
+          const uint32_t x = key(j, i);
+          if (i < end && x != 0xffffffffu && x >> above == at >> above) atomicAdd(&s_bins[mask - (int)(x >> shift & (uint32_t)mask)], 1);
+        });
+        __syncthreads();
       }
-      holes += __popcll(hole_lanes);
-      movers += __popcll(mover_lanes);
-    }
-    if (pass == 0) {
-      if (lane == 0) {
-        s_wave[0][wave] = holes;
-        s_wave[1][wave] = movers;
+      const int c0 = s_bins[2 * tid], c1 = s_bins[2 * tid + 1];
+      const int incl = wave_inclusive_scan(c0 + c1);
+      if (lane == 63) s_wave[1][wave] = incl;
+      __syncthreads();
+      s_bins[2 * tid] = s_bins[2 * tid + 1] = 0;
+      const int waves_incl = wave_inclusive_scan(over_waves(1));
+      const int before = incl - c0 - c1 + (wave > 0 ? __builtin_amdgcn_readlane(waves_incl, wave - 1) : 0);
+      if (before < ties && before + c0 + c1 >= ties) {
+        const bool first = before + c0 >= ties;
+        s_pick[0] = 2 * tid + (first ? 0 : 1);
+        s_pick[1] = before + (first ? 0 : c0);
       }
       __syncthreads();
-      for (int w = 0; w < kSelectWaves; ++w) {
-        free_before += w < wave ? s_wave[0][w] : 0;
-        move_before += w < wave ? s_wave[1][w] : 0;
-        count += s_wave[1][w];
-      }
+      at |= (uint32_t)((digit == 2 ? 1023 : 2047) - s_pick[0]) << shift;
+      ties -= s_pick[1];
     }
   }
-  if (tid == 0) moves[0] = count;
-  __syncthreads();  // the lists are written
-  for (int m = tid; m < count; m += kSelectThreads) {
-    const int to = moves[1 + m], from = moves[1 + a.most + m];
-    weights_out[to] = weights[from];
-    if (positions_out != nullptr) positions_out[to] = positions[from];
+
+  int equal = 0;
+  pieces([&](int j, int i) { equal += count_if(i < end && key(j, i) == at); });
+  if (lane == 0) s_wave[2][wave] = equal;
+  __syncthreads();
+  auto before_wave = [&](int which) {
+    const int incl = wave_inclusive_scan(over_waves(which));
+    return wave > 0 ? __builtin_amdgcn_readlane(incl, wave - 1) : 0;
+  };
+  const int ties_before = before_wave(2);
+  int tied = ties_before;
+  auto stays = [&](int j, int i) {  // called piece by piece
+    const uint32_t x = key(j, i);
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(i < end && x == at);
+    const bool yes = i < end && (x > at || (x == at && tied + lanes_below(eq) < ties));
+    tied += __popcll(eq);
+    return yes;
+  };
+  int holes = 0, movers = 0;
+  uint64_t staying[kHeld];  // registers: found once
+  pieces([&](int j, int i) {
+    const bool yes = stays(j, i);
+    if constexpr (kKeys > 0) staying[j] = __builtin_amdgcn_ballot_w64(yes);
+    holes += count_if(!yes && i < min(end, keep));
+    movers += count_if(yes && i >= keep);
+  });
+  if (lane == 0) {
+    s_wave[0][wave] = holes;
+    s_wave[1][wave] = movers;
   }
-  __syncthreads();  // (the outputs may be the arrays themselves)
-  for (int i = keep + tid; i < n; i += kSelectThreads) {
-    weights_out[i] = 0.f;
-    if (positions_out != nullptr) positions_out[i] = -1;
+  __syncthreads();
+  holes = before_wave(0);
+  movers = before_wave(1);
+  const int count = __builtin_amdgcn_readlane(wave_inclusive_scan(over_waves(1)), 63);
+  if (tid == 0) moves[0] = count;
+  // The free slots are listed; then who moves reads its slot, writes the pair down and its weight and position there.  Every slot's own weight and
+  // position are read by its own thread only, ahead of what it writes, so the outputs may be the arrays themselves: a free slot's are not needed.
+  const bool in_lds = count <= kHoleList;
+  tied = ties_before;
+  int at_hole = holes;
+  pieces([&](int j, int i) {
+    bool yes;
+    if constexpr (kKeys > 0) yes = staying[j] >> lane & 1u;
+    else yes = stays(j, i);
+    const bool hole = !yes && i < min(end, keep);
+    const uint64_t who = __builtin_amdgcn_ballot_w64(hole);
+    const int m = at_hole + lanes_below(who);
+    if (hole) (in_lds ? s_holes[m] : moves[2 + 2 * m]) = i;
+    at_hole += __popcll(who);
+  });
+  __syncthreads();
+  tied = ties_before;
+  int at_mover = movers;
+  pieces([&](int j, int i) {
+    bool yes;
+    if constexpr (kKeys > 0) yes = staying[j] >> lane & 1u;
+    else yes = stays(j, i);
+    const bool mover = yes && i >= keep;
+    const uint64_t who = __builtin_amdgcn_ballot_w64(mover);
+    const int m = at_mover + lanes_below(who);
+    at_mover += __popcll(who);
+    if (i < end) {
+      float w = 0.f;
+      int p = -1;
+      if (yes) {
+        if constexpr (kRemember) {
+          w = weight[j];
+          if (positions != nullptr) p = position[j];
+        } else {
+          w = weights[i];
+          if (positions != nullptr) p = positions[i];
+        }
+      }
+      if (mover) {
+        const int to = in_lds ? s_holes[m] : moves[2 + 2 * m];
+        *reinterpret_cast<i32x2*>(moves + 2 + 2 * m) = i32x2{to, i};
+        if (kKeys > 0) {
+          weights_out[to] = w;
+          if (positions_out != nullptr) positions_out[to] = p;
+        }
+      }
+      if (kKeys > 0 || i < keep) {
+        if (i >= keep || yes) {
+          weights_out[i] = i < keep ? w : 0.f;
+          if (positions_out != nullptr) positions_out[i] = i < keep ? p : -1;
+        }
+      }
+    }
+  });
+  if constexpr (kKeys == 0) {
+    // (keys were made from the arrays up to here: what changes a weight or a position that a key is made from comes after them all)
+    __syncthreads();
+    for (int m = tid; m < count; m += kSelectThreads) {
+      const int to = moves[2 + 2 * m], from = moves[3 + 2 * m];
+      weights_out[to] = weights[from];
+      if (positions_out != nullptr) positions_out[to] = positions[from];
+    }
+    __syncthreads();
+    for (int i = keep + tid; i < n; i += kSelectThreads) {
+      weights_out[i] = 0.f;
+      if (positions_out != nullptr) positions_out[i] = -1;
+    }
   }
 }
 
@@ -252,7 +340,7 @@ template <int kRowBytes>
 __global__ __launch_bounds__(256) void move_kernel(const EvictArgs a) {
   constexpr int kLanes = kRowBytes / 16, kRows = 256 / kLanes;  // lanes of a row, rows of a workgroup at a time
   const int bh = blockIdx.x, b = bh / a.kv_heads, h = bh % a.kv_heads;
-  const int32_t* moves = a.moves + (size_t)bh * (size_t)(1 + 2 * a.most);
+  const int32_t* moves = a.moves + (size_t)bh * (size_t)(2 + 2 * a.most);
   const int32_t* table = a.block_table + (size_t)b * a.table_pages;
   if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.new_lens[b] = min(clampi(a.ctx_lens[b], 0, a.max_len), a.budget);
   const int count = moves[0], piece = (int)threadIdx.x % kLanes;
@@ -261,8 +349,8 @@ __global__ __launch_bounds__(256) void move_kernel(const EvictArgs a) {
     return (((page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) + in_page) * (size_t)kLanes + (size_t)piece;
   };
   for (int m = (int)blockIdx.y * kRows + (int)threadIdx.x / kLanes; m < count; m += (int)gridDim.y * kRows) {
-    const int to = pool_row(table, moves[1 + m], a.page_shift, a.num_pages);
-    const int from = pool_row(table, moves[1 + a.most + m], a.page_shift, a.num_pages);
+    const i32x2 pair = *reinterpret_cast<const i32x2*>(moves + 2 + 2 * m);
+    const int to = pool_row(table, pair[0], a.page_shift, a.num_pages), from = pool_row(table, pair[1], a.page_shift, a.num_pages);
     if (to < 0 || from < 0) continue;
     const size_t src = place(from), dst = place(to);
     const u32x4 kx = __builtin_nontemporal_load(a.k + src), vx = __builtin_nontemporal_load(a.v + src);
@@ -341,9 +429,12 @@ extern "C" int paged_evict(const span_paged_desc_t* desc, void* k_pages, void* v
   a.most = a.max_len > a.budget ? (a.max_len - a.budget < a.budget ? a.max_len - a.budget : a.budget) : 0;
   const unsigned pairs = (unsigned)desc->batch * (unsigned)desc->kv_heads;
   hipStream_t stream = (hipStream_t)desc->stream;
-  constexpr int kSmall = 8192, kLarge = 32768;
-  if (a.max_len <= kSmall) hipLaunchKernelGGL(select_kernel<kSmall>, dim3(pairs), dim3(kSelectThreads), 0, stream, a);
-  else hipLaunchKernelGGL(select_kernel<kLarge>, dim3(pairs), dim3(kSelectThreads), 0, stream, a);
+  auto select = [&](auto keys) { hipLaunchKernelGGL(select_kernel<decltype(keys)::value>, dim3(pairs), dim3(kSelectThreads), 0, stream, a); };
+  if (a.max_len <= 2 * kSelectThreads) select(std::integral_constant<int, 2>{});
+  else if (a.max_len <= 8 * kSelectThreads) select(std::integral_constant<int, 8>{});
+  else if (a.max_len <= 16 * kSelectThreads) select(std::integral_constant<int, 16>{});
+  else if (a.max_len <= 32 * kSelectThreads) select(std::integral_constant<int, 32>{});
+  else select(std::integral_constant<int, 0>{});
   const int src = launched();
   if (src != SPAN_OK) return src;
   const int row_bytes = desc->head_dim * (desc->dtype == SPAN_F32 ? 4 : 2), rows = 256 / (row_bytes / 16);
