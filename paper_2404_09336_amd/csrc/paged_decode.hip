@@ -22,11 +22,14 @@ struct PagedArgs : LaunchArgs {  // heads: KV heads; max_len: positions of a seq
   int32_t table_pages, page_shift, num_pages;
   int32_t group;             // query heads per KV head
   int32_t batch, window, sinks;
-  int32_t room;              // > 0: slices per head aimed at, see locate_slice; 0: num_splits each, or the table
+  int32_t room, more_room;   // > 0: slices per head aimed at, see locate_slice; 0: num_splits each, or the table
+  int32_t whole;             // up to so many positions a sequence is not cut
   float* scores;             // [batch, kv head, query head of the group, max_len] unscaled scores by virtual position, or null
   float* final_ml;           // [batch, query head] (maximum, sum)
   int32_t* counts;           // span form with weights: [batch] attended positions
   int32_t* list;             // ... and [batch, max_len] the positions themselves
+  float* weights;
+  int32_t weights_here;      // 1: the workgroup that attends adds up the weights too (every pair is one workgroup)
 };
 struct PagedArgsPlain : PagedArgs {
   static constexpr bool kHasTable = false;
@@ -42,35 +45,65 @@ struct PagedShape {
   static constexpr int NK = kRowBytes / 64;        // 16-byte pieces of a K row per lane
   static constexpr int NE = D / 16;                // values of a V row per lane
   static constexpr int VW = NE * Elt::kBytes / 4;  // dwords they fill: 2, 4, or 8 (fp32, D = 128: two pieces)
-  static constexpr int S = Elt::kBytes == 2 && D == 64 ? 2 : 1;  // groups of 16 rows in a tile
-  static constexpr int kWaves = Elt::kBytes == 4 && D == 128 ? 2 : 4;  // per SIMD
+  // Groups of 16 rows in a step.  More of them, with fewer waves (two of 256-byte rows at three per SIMD, four at two), are slower: a call of few
+  // positions by its longer code, one of many by the waves (31 drawn and listed calls, mean 12.2 us -> 12.9 and 14.4).
+  static constexpr int S = kRowBytes == 128 ? 2 : 1;
+  static constexpr int kWaves = kRowBytes == 512 ? 2 : 4;  // per SIMD
 };
 
 struct Slice {
   int b, split, nsl, y0, len;  // sequence, slice within it, slices of it, slot of its first slice; its length (locate_slice)
 };
 
-// Slices of a dense call: sequence b has ceil(n_b / T) (one at least), T = the positions of all sequences over `room`, of whole tiles and
-// kPagedLeastSlice at least, so there are room + batch at most.  Row y of the grid is the y-th of them.  Every workgroup works it out for
-// itself: one load of the lengths, which it needs anyway, and two scans for up to 64 sequences.
+// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than kPagedWhole, T whole steps and
+// kPagedLeastSlice at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
+// many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice well above the
+// mean, which is what the whole call waits for then, `more_room` is tried.  Every workgroup works it out for itself: one load of the lengths,
+// which it needs anyway, and a few scans for up to 64 sequences.
+// (us, 1024 workgroups always -> 512 and 1024 where those are not level: 32 sequences in a window of 1024 29.0 -> 27.0, four of 8000 .. 32768 72.9 -> 68.7;
+// 512 always: 64 x 8 pairs of 512 .. 4096 106.4 -> 112.2.  One round each way: with as many slices as came out, 1.25 rounds, those took 110.9.)
 __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lane) {
-  uint32_t all = 0;
   int len = 0, n = 0;
   auto fetch = [&](int c) {
     len = c + lane < a.batch ? clampi(a.ctx_lens[c + lane], 0, a.max_len) : 0;
     n = seen_by_last(len, a.window, a.sinks).count;
   };
+  uint32_t all = 0, longest = 1;
   for (int c = 0; c < a.batch; c += 64) {
     fetch(c);
     all += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(n), 63);
+    longest = max(longest, (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_max(n), 63));
   }
-  const uint32_t even = (all + (uint32_t)a.room - 1u) / (uint32_t)a.room;
-  const uint32_t T = max((even + kPagedSliceStep - 1u) / kPagedSliceStep * kPagedSliceStep, (uint32_t)kPagedLeastSlice);
+  auto steps = [](uint32_t x) { return (x + kPagedSliceStep - 1u) / kPagedSliceStep * kPagedSliceStep; };
+  auto slices = [&](uint32_t T) { return n > a.whole ? (int)(((uint32_t)n + T - 1u) / T) : 1; };  // of this lane's sequence
+  const uint32_t batch = (uint32_t)a.batch;
+  uint32_t T = longest;
+  if (longest > (uint32_t)a.whole) {
+#pragma unroll 1
+    for (int pass = 0; pass < 2; ++pass) {
+      const uint32_t room = (uint32_t)(pass == 0 ? a.room : a.more_room);
+      T = longest;
+      if (room > batch) {
+        const float mean = (float)all / ((float)room - 0.5f * (float)batch);  // (a sequence has half a slice more than its share on average)
+        T = max(steps((uint32_t)mean), (uint32_t)kPagedLeastSlice);
+        while (T < longest) {
+          uint32_t total = 0;
+          for (int c = 0; c < a.batch; c += 64) {
+            if (a.batch > 64) fetch(c);
+            total += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(c + lane < a.batch ? slices(T) : 0), 63);
+          }
+          if (total <= room) break;
+          T = min(max(steps((uint32_t)((float)T * (float)total / (float)room)), steps(T + T / 16)), longest);
+        }
+      }
+      if ((float)min(T, longest) * (float)max(room, batch) <= 1.4f * (float)all || T <= (uint32_t)kPagedLeastSlice) break;
+    }
+  }
   Slice s = {-1, 0, 1, 0, 0};
   int before = 0;
   for (int c = 0; c < a.batch; c += 64) {
     if (a.batch > 64) fetch(c);
-    const int nsl = c + lane < a.batch ? max((int)(((uint32_t)n + T - 1u) / T), 1) : 0;
+    const int nsl = c + lane < a.batch ? slices(T) : 0;
     const int incl = before + wave_inclusive_scan(nsl);
     const uint64_t past = __builtin_amdgcn_ballot_w64(incl > y);
     if (past != 0) {
@@ -87,12 +120,51 @@ __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lan
   return s;
 }
 
-template <class Elt, int D, bool kSpans, class Args>
+// weights[b, h, p] += sum over the group's heads of exp2((score - maximum) * post) / sum, for the positions with virtual numbers v0 .. v0 + 3.  A
+// position is one thread's, so the sums do not depend on any order.
+template <class Elt, bool kSpans>
+__device__ __forceinline__ void add_weights(const PagedArgs& a, const Seen& seen, int n, int b, int h, int v0) {
+  const float post = Elt::post_scale(a.scale_log2e);
+  const size_t bh = (size_t)b * a.heads + h;
+  f32x4 w = {0.f, 0.f, 0.f, 0.f};
+  for (int g = 0; g < a.group; ++g) {
+    const size_t head = bh * (size_t)a.group + (size_t)g;
+    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.final_ml + 2 * head);
+    const f32x4 s = *reinterpret_cast<const f32x4*>(a.scores + head * (size_t)a.max_len + (size_t)v0);
+    const float inv = ml[1] != 0.f ? 1.f / ml[1] : 0.f;
+    const float safe = ml[0] == -INFINITY ? 0.f : ml[0];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = fmaf(__builtin_amdgcn_exp2f((s[k] - safe) * post), inv, w[k]);
+  }
+  float* row = a.weights + bh * (size_t)a.max_len;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int v = v0 + k;
+    if (v < n) {
+      const int p = kSpans ? a.list[(size_t)b * a.max_len + v] : (v < seen.sinks ? v : v - seen.sinks + seen.low);
+      row[p] += w[k];
+    }
+  }
+}
+
+// A wave's instruction priority falls as it gets on with its rows.  Among equals a SIMD issues the oldest wave first, and the workgroups that arrive last on
+// a CU got their first rows when the others were nearly done (stamps: after 5 to 67 us of a call of 107), to end alone.  64 x 8 pairs of 512 .. 4096
+// 107.1 -> 104.6; smaller calls 0 to 1 %.
+__device__ __forceinline__ void priority(int done, int quarter) {
+  if (done == 0) __builtin_amdgcn_s_setprio(3);
+  else if (done == quarter) __builtin_amdgcn_s_setprio(2);
+  else if (done == 2 * quarter) __builtin_amdgcn_s_setprio(1);
+  else if (done == 3 * quarter) __builtin_amdgcn_s_setprio(0);
+}
+
+// kWeights: a call that adds up weights.  (Code that is jumped over is fetched all the same: without weights the few microseconds of the smallest calls
+// are 0.3 to 0.7 shorter for its absence.)
+template <class Elt, int D, bool kSpans, bool kWeights, class Args>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D>::kWaves))) void paged_kernel(const Args a) {
   using Shape = PagedShape<Elt, D>;
   constexpr int NK = Shape::NK, NE = Shape::NE, VW = Shape::VW, S = Shape::S;
-  constexpr int TR = 16 * S;  // rows of a tile
+  constexpr int TR = 16 * S;  // rows of a step
   constexpr uint32_t ROWB = Shape::kRowBytes;
   constexpr int kPieces = ROWB / 16;
   constexpr int kQRow = ROWB + 16;  // LDS rows of q, padded: operand reads spread over the banks
@@ -102,6 +174,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
   constexpr bool kSplitPieces = VW == 8;
   static_assert(kPWin % TR == 0, "tiles do not straddle a window");
 
+  priority(0, 0);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qi = lane & 15, c4 = lane >> 4;
@@ -175,21 +248,22 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
   const int T = (int)(((uint32_t)(n_total + nsl - 1) / (uint32_t)nsl + kPagedSliceStep - 1) / kPagedSliceStep * kPagedSliceStep);
   const int slice_begin = min((int)min((int64_t)split * T, (int64_t)n_total), n_total);
   const int cnt = __builtin_amdgcn_readfirstlane(min(n_total - slice_begin, T));
-  if (kSpans && a.counts != nullptr && split == 0 && h == 0 && tid == 0) a.counts[b] = n_total;
+  if (kSpans && kWeights && split == 0 && h == 0 && tid == 0) a.counts[b] = n_total;
 
-  // Tiles are dealt to the waves round-robin: wave w has the slice's tiles w, w + 4, ...
-  const int units_all = (cnt + TR - 1) / TR;
+  // Units of 16 rows are dealt to the waves round-robin (wave w has the slice's units w, w + 4, ...), which take S of them at a step.
+  constexpr int kUnit = 16;
+  const int units_all = (cnt + kUnit - 1) / kUnit;
   const int units = units_all > wave ? (units_all - wave + kWavesPerBlock - 1) / kWavesPerBlock : 0;
   const bool own_last = units > 0 && wave + (units - 1) * kWavesPerBlock == units_all - 1;
-  const int nrows = units * TR - (own_last ? units_all * TR - cnt : 0);
-  const int vbase = slice_begin + wave * TR;
-  constexpr int kGap = (kWavesPerBlock - 1) * TR;
-  auto vrow = [&](int r) { return vbase + r + (r / TR) * kGap; };
+  const int nrows = units * kUnit - (own_last ? units_all * kUnit - cnt : 0);
+  const int vbase = slice_begin + wave * kUnit;
+  constexpr int kGap = (kWavesPerBlock - 1) * kUnit;
+  auto vrow = [&](int r) { return vbase + r + (r / kUnit) * kGap; };
 
-  // Pool rows of the wave's rows w0 .. w0 + wn - 1, and -1 up to the end of their last tile.
+  // Pool rows of the wave's rows w0 .. w0 + wn - 1, and -1 up to the end of their last step.
   auto tabulate = [&](int w0, int wn, int ln) {
     if constexpr (kSpans) {
-      if (w0 == 0 && intervals.count <= 64) tabulate_short<TR, kPWin>(a, intervals, vbase, kGap, wn, wave, ln, s_u.st.tab, s_row[wave]);
+      if (w0 == 0 && intervals.count <= 64) tabulate_short<kUnit, kPWin>(a, intervals, vbase, kGap, wn, wave, ln, s_u.st.tab, s_row[wave]);
       else tabulate_positions(a, intervals, vrow, w0, wn, wave, ln, s_u.st.tab, s_row[wave]);
     }
     const int padded = (wn + TR - 1) / TR * TR;
@@ -201,7 +275,8 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         if constexpr (kSpans) p = s_row[wave][r];
         else p = v < seen.sinks ? v : v - seen.sinks + seen.low;
         x = pool_row(table, p, a.page_shift, a.num_pages);
-        if (kSpans && a.list != nullptr && h == 0) a.list[(size_t)b * a.max_len + v] = p;
+        // (who adds up weights reads his own entries back; the heads' are equal)
+        if (kSpans && kWeights && (h == 0 || a.weights_here)) a.list[(size_t)b * a.max_len + v] = p;
       }
       s_row[wave][r] = x;
     }
@@ -307,23 +382,26 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         for (int s = 0; s < S; ++s) sc[s] += Elt::mfma(kr[s][mm], qm, kZero);
       }
     } else {
-      f32x4 sum[4] = {kZero, kZero, kZero, kZero};
 #pragma unroll
-      for (int mm = 0; mm < NK; ++mm) {
-        const u32x4 qm = *reinterpret_cast<const u32x4*>(qrow_lds + 64 * mm);
-        f32x4 piece[2] = {kZero, kZero};
+      for (int s = 0; s < S; ++s) {
+        f32x4 sum[4] = {kZero, kZero, kZero, kZero};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t kw = kr[0][mm][k], qw = qm[k];
-          piece[k & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kw), __builtin_bit_cast(float, qw), piece[k & 1], 0, 0, 0);
+        for (int mm = 0; mm < NK; ++mm) {
+          const u32x4 qm = *reinterpret_cast<const u32x4*>(qrow_lds + 64 * mm);
+          f32x4 piece[2] = {kZero, kZero};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t kw = kr[s][mm][k], qw = qm[k];
+            piece[k & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, kw), __builtin_bit_cast(float, qw), piece[k & 1], 0, 0, 0);
+          }
+          sum[mm & 3] += piece[0] + piece[1];
         }
-        sum[mm & 3] += piece[0] + piece[1];
+        sc[s] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        pin(sc[s]);
       }
-      sc[0] = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-      pin(sc[0]);
     }
   };
-  // Scores -> weights; moves the state's maximum and adds to its sum.  v0: virtual position of the tile's first row.
+  // Scores -> weights; moves the state's maximum and adds to its sum.  v0: virtual position of the step's first row.
   auto softmax_step = [&](f32x4 (&sc)[S], int v0, const TileRows& tr) {
     if (!tr.plain) {
 #pragma unroll
@@ -332,12 +410,13 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         for (int t = 0; t < 4; ++t) sc[s][t] = (tr.ok[s] >> (4 * c4 + t)) & 1u ? sc[s][t] : -INFINITY;
       }
     }
-    if (a.scores != nullptr && qi < group) {
+    if (kWeights && qi < group) {
       float* at = a.scores + (bh * (size_t)group + (size_t)qi) * (size_t)a.max_len + (size_t)(v0 + 4 * c4);
 #pragma unroll
       for (int s = 0; s < S; ++s) {
         // (a quad that begins past the last position belongs to nobody, or to the next slice)
-        if (v0 + 16 * s + 4 * c4 < slice_begin + cnt) *reinterpret_cast<f32x4*>(at + 16 * s) = sc[s];
+        const int v = kWavesPerBlock * kUnit * s;  // the wave's next unit
+        if (v0 + v + 4 * c4 < slice_begin + cnt) *reinterpret_cast<f32x4*>(at + v) = sc[s];
       }
     }
     float mx = -INFINITY;
@@ -398,8 +477,11 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         f32x4 part = D == 64 ? f32x4{0.f, 0.f, 0.f, 0.f} : O[e];
 #pragma unroll
         for (int i = kTerms - 1; i >= 0; --i) {
-          if constexpr (S == 2) part = Elt::mfma(u32x4{va[0], va[1], va[2], va[3]}, u32x4{terms[i][0], terms[i][1], terms[i][2], terms[i][3]}, part);
-          else part = Elt::mfma(u32x2{va[0], va[1]}, u32x2{terms[i][0], terms[i][1]}, part);
+          if constexpr (S == 1) part = Elt::mfma(u32x2{va[0], va[1]}, u32x2{terms[i][0], terms[i][1]}, part);
+#pragma unroll
+          for (int s = 0; s + 1 < S; s += 2)
+            part = Elt::mfma(u32x4{va[2 * s], va[2 * s + 1], va[2 * s + 2], va[2 * s + 3]},
+                             u32x4{terms[i][2 * s], terms[i][2 * s + 1], terms[i][2 * s + 2], terms[i][2 * s + 3]}, part);
         }
         O[e] = D == 64 ? O[e] + part : part;
         if (D == 64) pin(O[e]);
@@ -409,9 +491,12 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
       for (int e = 0; e < NE; ++e) {
         f32x4 part[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t vw = vr[0][t][e];
-          part[t & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vw), w[0][t], part[t & 1], 0, 0, 0);
+        for (int s = 0; s < S; ++s) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const uint32_t vw = vr[s][t][e];
+            part[t & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, vw), w[s][t], part[t & 1], 0, 0, 0);
+          }
         }
         O[e] += part[0] + part[1];
         pin(O[e]);
@@ -432,6 +517,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     *reinterpret_cast<u32x4*>(&s_q[j * kQRow + 16u * (uint32_t)(idx % kPieces)]) = q_piece[i];
   }
   __syncthreads();  // q is in LDS
+  const int quarter = max((nrows / 4 + TR - 1) / TR * TR, TR);
   for (int w0 = 0; w0 < nrows; w0 += kPWin) {
     const int wn = min(kPWin, nrows - w0);
     if (__builtin_expect(w0 > 0, 0)) {
@@ -444,6 +530,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     int base = 0;
     for (; base + TR < wn; base += TR) {
       f32x4 sc[S];
+      if (w0 + base > 0) priority(w0 + base, quarter);
       take_scores(sc);
       const TileRows next = load_k(base + TR, lane);
       softmax_step(sc, vrow(w0 + base), cur);
@@ -472,7 +559,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     float* row = a.out + qrow(mine) * D + 4 * part;
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) *reinterpret_cast<f32x4*>(row + 4 * kPerToken * i) = f32x4{o[i][0] / sum, o[i][1] / sum, o[i][2] / sum, o[i][3] / sum};
-    if (a.final_ml != nullptr && part == 0) *reinterpret_cast<f32x2*>(a.final_ml + 2 * qrow(mine)) = f32x2{M, L / Elt::kWeightScale};
+    if (kWeights && part == 0) *reinterpret_cast<f32x2*>(a.final_ml + 2 * qrow(mine)) = f32x2{M, L / Elt::kWeightScale};
   };
   __syncthreads();  // the (maximum, sum) pairs are in LDS; the streaming tables are no longer read
   if (qi < group) {
@@ -519,7 +606,13 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
       if (part == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{M, L}), ml_slot(my_slot), (uint32_t)mine * 8u, 0, kThrough);
     }
   }
-  if (direct) return;
+  if (direct) {
+    if (kWeights && a.weights_here) {  // (no sequence of the call is cut: nothing else is waited for)
+      __syncthreads();     // scores, list and final states are written
+      for (int v0 = 4 * tid; v0 < n_total; v0 += 4 * kThreads) add_weights<Elt, kSpans>(a, seen, n_total, b, h, v0);
+    }
+    return;
+  }
 
   // ---- several slices: the workgroup that arrives last for the pair merges them all (the hand-over of matrix_kernel) ----
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // my published stores are acknowledged
@@ -576,10 +669,8 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
   if (tid == 0) __hip_atomic_store(a.counters + bh * (size_t)a.counter_stride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// weights[b, h, p] += sum over the group's heads of exp2((score - maximum) * post) / sum, for the positions p that the call attended.
-// A thread has four positions; a position is one thread's, so the sums do not depend on any order.
 template <class Elt, bool kSpans>
-__global__ __launch_bounds__(256) void weights_kernel(const PagedArgs a, float* weights) {
+__global__ __launch_bounds__(256) void weights_kernel(const PagedArgs a) {
   const int h = blockIdx.y, b = blockIdx.z;
   const int v0 = 4 * (int)(blockIdx.x * 256 + threadIdx.x);
   Seen seen = {0, 0, 0};
@@ -589,28 +680,7 @@ __global__ __launch_bounds__(256) void weights_kernel(const PagedArgs a, float* 
     seen = seen_by_last(clampi(a.ctx_lens[b], 0, a.max_len), a.window, a.sinks);
     n = seen.count;
   }
-  if (v0 >= n) return;
-  const float post = Elt::post_scale(a.scale_log2e);
-  const size_t bh = (size_t)b * a.heads + h;
-  f32x4 w = {0.f, 0.f, 0.f, 0.f};
-  for (int g = 0; g < a.group; ++g) {
-    const size_t head = bh * (size_t)a.group + (size_t)g;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.final_ml + 2 * head);
-    const f32x4 s = *reinterpret_cast<const f32x4*>(a.scores + head * (size_t)a.max_len + (size_t)v0);
-    const float inv = ml[1] != 0.f ? 1.f / ml[1] : 0.f;
-    const float safe = ml[0] == -INFINITY ? 0.f : ml[0];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] = fmaf(__builtin_amdgcn_exp2f((s[k] - safe) * post), inv, w[k]);
-  }
-  float* row = weights + bh * (size_t)a.max_len;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int v = v0 + k;
-    if (v < n) {
-      const int p = kSpans ? a.list[(size_t)b * a.max_len + v] : (v < seen.sinks ? v : v - seen.sinks + seen.low);
-      row[p] += w[k];
-    }
-  }
+  if (v0 < n) add_weights<Elt, kSpans>(a, seen, n, b, h, v0);
 }
 
 __global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* p, size_t n) {
@@ -621,11 +691,12 @@ __global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* p, size_t n)
 size_t counter_bytes(const span_paged_desc_t* d) { return ((size_t)d->batch * d->kv_heads * sizeof(int32_t) + 255) & ~(size_t)255; }
 
 template <class Elt, int D, bool kSpans>
-int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, float* weights, hipStream_t stream) {
+int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, hipStream_t stream) {
   const dim3 grid((unsigned)base.heads, (unsigned)p.rows);
   auto start = [&](const auto& a) {
     using Args = std::decay_t<decltype(a)>;
-    hipLaunchKernelGGL((paged_kernel<Elt, D, kSpans, Args>), grid, dim3(kThreads), 0, stream, a);
+    if (a.weights != nullptr) hipLaunchKernelGGL((paged_kernel<Elt, D, kSpans, true, Args>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((paged_kernel<Elt, D, kSpans, false, Args>), grid, dim3(kThreads), 0, stream, a);
   };
   PagedArgsPlain plain;
   static_cast<PagedArgs&>(plain) = base;
@@ -642,11 +713,11 @@ int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, 
     start(plain);
   }
   const int rc = launched();
-  if (rc != SPAN_OK || weights == nullptr) return rc;
+  if (rc != SPAN_OK || base.weights == nullptr || base.weights_here) return rc;
   int64_t most = base.max_len;
   if (!kSpans && base.window > 0 && (int64_t)base.window + base.sinks < most) most = (int64_t)base.window + base.sinks;
   hipLaunchKernelGGL((weights_kernel<Elt, kSpans>), dim3((unsigned)((most + 1023) / 1024), (unsigned)base.heads, (unsigned)base.batch), dim3(256), 0,
-                     stream, base, weights);
+                     stream, base);
   return launched();
 }
 
@@ -689,19 +760,23 @@ int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const
   a.window = d->window;
   a.sinks = d->sinks;
   a.room = p.room;
+  a.more_room = p.rows;
+  a.whole = paged_whole(d);
   a.final_ml = weights ? (float*)(at + w.final_ml) : nullptr;
   a.counts = weights && kSpans ? (int32_t*)(at + w.counts) : nullptr;
   a.list = weights && kSpans ? (int32_t*)(at + w.list) : nullptr;
   a.scores = weights ? (float*)(at + w.scores) : nullptr;
+  a.weights = weights;
+  a.weights_here = weights && !w.sliced ? 1 : 0;
   hipStream_t stream = (hipStream_t)d->stream;
   const bool d128 = d->head_dim == 128;
   switch (d->dtype) {
     case SPAN_F32:
-      return d128 ? run_paged<F32, 128, kSpans>(a, p, table, weights, stream) : run_paged<F32, 64, kSpans>(a, p, table, weights, stream);
+      return d128 ? run_paged<F32, 128, kSpans>(a, p, table, stream) : run_paged<F32, 64, kSpans>(a, p, table, stream);
     case SPAN_F16:
-      return d128 ? run_paged<F16, 128, kSpans>(a, p, table, weights, stream) : run_paged<F16, 64, kSpans>(a, p, table, weights, stream);
+      return d128 ? run_paged<F16, 128, kSpans>(a, p, table, stream) : run_paged<F16, 64, kSpans>(a, p, table, stream);
     default:
-      return d128 ? run_paged<BF16, 128, kSpans>(a, p, table, weights, stream) : run_paged<BF16, 64, kSpans>(a, p, table, weights, stream);
+      return d128 ? run_paged<BF16, 128, kSpans>(a, p, table, stream) : run_paged<BF16, 64, kSpans>(a, p, table, stream);
   }
 }
 

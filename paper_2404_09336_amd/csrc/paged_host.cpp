@@ -25,14 +25,13 @@ int check_paged(const span_paged_desc_t* d) {
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
-// Workgroups a one-token call aims at.
-constexpr int64_t kPagedWorkgroups = 1024;
-
-static int64_t slice_room(const span_paged_desc_t* d) { return std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads); }
+// Workgroups a one-token call aims at: two per CU, and as many as run at once (four) where that leaves slices of very different length.
+constexpr int64_t kPagedWorkgroups = 512, kPagedMoreWorkgroups = 1024;
 
 PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
   PagedPlan p = {0, 1, false, 0};
-  const int64_t cap = capacity(d), room = slice_room(d);
+  const int64_t cap = capacity(d), whole = paged_whole(d);
+  const int64_t room = std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads), more_room = std::max<int64_t>(1, kPagedMoreWorkgroups / d->kv_heads);
   auto uniform = [&](int64_t splits) {
     splits = std::min(splits, ceil_div(cap, kPagedSliceStep));
     splits = std::min<int64_t>(splits, 65535 / d->batch);  // grid.y
@@ -44,22 +43,38 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
   if (!spans) {
     if (d->batch > kPagedLocateBatch) return uniform(1);
     const int64_t most = d->window > 0 ? std::min<int64_t>(cap, (int64_t)d->window + d->sinks) : cap;  // positions of any sequence
-    if (most <= kPagedLeastSlice) return uniform(1);
+    if (most <= whole) return uniform(1);
     p.room = (int32_t)room;
     p.splits = 2;
-    p.rows = (int32_t)std::min<int64_t>(room + d->batch, ceil_div(most, kPagedLeastSlice) * d->batch);
+    p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(most, kPagedLeastSlice) * d->batch));
     return p;
   }
-  if (d->tokens_per_seq && d->batch <= kMaxPlanSlices) {
+  if (d->tokens_per_seq && d->batch <= kMaxPlanSlices) {  // as locate_slice does
     auto tokens = [&](int32_t b) { return std::min(std::max<int64_t>(d->tokens_per_seq[b], 0), cap); };
-    int64_t sum = 0;
-    for (int32_t b = 0; b < d->batch; ++b) sum += tokens(b);
-    // at most room + batch slices; the table's entries bound them
-    const int64_t aim = std::max<int64_t>(1, std::min<int64_t>(room, kMaxPlanSlices - d->batch));
-    const int64_t T = std::max<int64_t>(kPagedLeastSlice, round_up(ceil_div(sum, aim), kPagedSliceStep));
+    int64_t sum = 0, longest = 1;
+    for (int32_t b = 0; b < d->batch; ++b) {
+      sum += tokens(b);
+      longest = std::max(longest, tokens(b));
+    }
+    int64_t T = longest;
+    auto slices = [&](int32_t b) { return tokens(b) > whole ? ceil_div(tokens(b), T) : 1; };
+    for (const int64_t aim : {room, more_room}) {
+      const int64_t most = std::min<int64_t>(aim, kMaxPlanSlices);
+      T = longest;
+      if (most > d->batch) {
+        T = std::max<int64_t>(kPagedLeastSlice, round_up(2 * sum / (2 * most - d->batch), kPagedSliceStep));
+        while (T < longest) {
+          int64_t total = 0;
+          for (int32_t b = 0; b < d->batch; ++b) total += slices(b);
+          if (total <= most) break;
+          T = std::min(std::max(round_up(T * total / most, kPagedSliceStep), round_up(T + T / 16, kPagedSliceStep)), longest);
+        }
+      }
+      if (std::min(T, longest) * std::max<int64_t>(most, d->batch) * 5 <= 7 * sum || T <= kPagedLeastSlice) break;
+    }
     int64_t most = 1, least = kMaxPlanSplits, y = 0;
     for (int32_t b = 0; b < d->batch; ++b) {
-      const int64_t nsl = std::max<int64_t>(1, ceil_div(tokens(b), T));
+      const int64_t nsl = slices(b);
       most = std::max(most, nsl);
       least = std::min(least, nsl);
       y += nsl;
@@ -69,7 +84,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
       if (table) {
         int32_t at = 0;
         for (int32_t b = 0; b < d->batch; ++b) {
-          const int64_t nsl = std::max<int64_t>(1, ceil_div(tokens(b), T));
+          const int64_t nsl = slices(b);
           for (int64_t s = 0; s < nsl; ++s) table[at++] = pack_slice((uint32_t)b, (uint32_t)s, (uint32_t)nsl);
         }
       }
@@ -131,10 +146,10 @@ size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p) {
   return p.acc + (size_t)p.tiles * d->kv_heads * p.splits * kPromptTileRows * d->head_dim * sizeof(float);
 }
 
-// Of every (sequence, KV head) the number of rows that move and their slots, from and to.
+// Of every (sequence, KV head) the number of rows that move and the pairs of their slots (8 bytes each).
 size_t evict_workspace(const span_paged_desc_t* d) {
   const size_t most = (size_t)std::min(d->budget, std::max(capacity(d) - d->budget, 0));
-  return (((size_t)d->batch * d->kv_heads * (1 + 2 * most) * sizeof(int32_t)) + 255) & ~(size_t)255;
+  return (((size_t)d->batch * d->kv_heads * (2 + 2 * most) * sizeof(int32_t)) + 255) & ~(size_t)255;
 }
 
 }  // namespace spanattn

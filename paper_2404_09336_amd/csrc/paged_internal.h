@@ -14,6 +14,9 @@ constexpr int kPagedLeastSlice = 128;  // do not cut finer: a tile per wave
 // takes longer than it gains, and there are workgroups enough without slices.
 constexpr int kPagedLocateBatch = 512;
 
+// A sequence of up to so many positions is not cut: the hand-over costs more than a workgroup's two or four tiles a wave.
+inline int32_t paged_whole(const span_paged_desc_t* d) { return d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
+
 int check_paged(const span_paged_desc_t* d);
 
 inline int page_shift(const span_paged_desc_t* d) { return __builtin_ctz((unsigned)d->page_size); }
@@ -21,7 +24,7 @@ inline int32_t capacity(const span_paged_desc_t* d) { return d->table_pages * d-
 
 // How a one-token call is cut.
 struct PagedPlan {
-  int32_t room;      // > 0: slices per head the kernel aims at over all sequences (locate_slice), rows = room + batch
+  int32_t room;      // > 0: slices per head the kernel aims at over all sequences (locate_slice; `rows` where that is not level)
   int32_t splits;    // room 0: slices of every sequence, or the most of any (table)
   bool table;        // slices from a table of pack_slice entries
   int32_t rows;      // grid.y: slices of all sequences (upper bound)

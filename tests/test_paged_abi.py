@@ -125,23 +125,37 @@ def test_prompts_without_tokens_and_with_too_many():
     assert call("paged_prompt_attn", desc(num_tokens=65536 * 32), *[FAR] * 6, 1.0, FAR) == -2  # tiles of 32 tokens of 4 heads: the grid's limit
 
 
-def slices(lens, room):
+def slices(lens, rooms, whole):
     """Slices of a dense call as the kernel finds them."""
-    T = max(-(-(-(-sum(lens) // room)) // 32) * 32, 128)
-    return sum(max(-(-n // T), 1) for n in lens)
+    total = lambda T: sum(1 if n <= whole else -(-n // T) for n in lens)  # noqa: E731
+    longest, T = max(max(lens), 1), max(max(lens), 1)
+    if longest <= whole:
+        return len(lens)
+    for room in rooms:
+        T = longest
+        if room > len(lens):
+            T = max(-(-int(sum(lens) / (room - 0.5 * len(lens))) // 32) * 32, 128)
+            while T < longest and total(T) > room:
+                T = min(max(-(-int(T * total(T) / room) // 32) * 32, -(-(T + T // 16) // 32) * 32), longest)
+        if min(T, longest) * max(room, len(lens)) <= 1.4 * sum(lens) or T <= 128:
+            break
+    return total(T)
 
 
 def test_the_grid_holds_every_slice():
     """The workspace has a state for every slice that any lengths give."""
     rng = np.random.default_rng(0)
-    for B, KV, G, D, TP in itertools.product([1, 2, 17, 64, 200, 512], [1, 3, 8, 32], [1, 4], [64, 128], [9, 40, 700]):
+    for B, KV, G, D, TP in itertools.product([1, 2, 17, 64, 200, 512], [1, 3, 8, 32], [1, 4], [64, 128], [9, 17, 40, 700]):
         d = desc(batch=B, heads=KV * G, kv_heads=KV, head_dim=D, table_pages=TP, num_pages=1 << 20)
         need = paged.paged_workspace_bytes(d, paged.PAGED_DECODE)
+        if TP * 16 <= 256:
+            assert need == 0                       # nothing to cut
+            continue
         counters = -(-B * KV * 4 // 256) * 256
         rows = (need - counters) // (KV * G * (D + 2) * 4)
-        room = max(1, 1024 // KV)
-        for lens in ([TP * 16] * B, [0] * B, [1] * (B - 1) + [TP * 16], list(rng.integers(0, TP * 16 + 1, B))):
-            assert slices([int(n) for n in lens], room) <= rows, (B, KV, TP)
+        rooms = max(1, 512 // KV), rows
+        for lens in ([TP * 16] * B, [0] * B, [1] * (B - 1) + [TP * 16], [257] * B, list(rng.integers(0, TP * 16 + 1, B))):
+            assert slices([int(n) for n in lens], rooms, 256) <= rows, (B, KV, TP)
 
 
 def test_binding_refuses_host_tensors():
