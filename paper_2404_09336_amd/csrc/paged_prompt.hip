@@ -49,8 +49,8 @@ struct PromptShape {
   static constexpr int kRowsPerWave = KT / kPromptWaves;
   static constexpr int kLoads = kRowsPerWave * kRowBytes / 1024;  // 16-byte loads per lane of K (and of V) for a tile
   static constexpr int kKRow = kRowBytes + 16;
-  // 16 bits: a row per dimension, 16-byte pieces of 8 positions, piece p of dimension d at p ^ (d / 8 % 8) (writes of 8 bytes then meet in
-  // no bank more often than they must); fp32: a row per position, rows 4 apart half the banks apart
+  // 16 bits: a row per dimension, 16-byte pieces of 8 positions, piece p of dimension d at p ^ (d / 16 % 8): 16 lanes that read a piece of 16 rows, or
+  // write 8 bytes of it each for 16 units of dimensions, then meet in no bank twice.  fp32: a row per position, rows 4 apart half the banks apart
   static constexpr int kVRow = kHalf ? KT * 2 + 16 : kRowBytes + 32;
   static constexpr int kKBytes = KT * kKRow, kVBytes = kHalf ? D * kVRow : KT * kVRow;
 };
@@ -105,6 +105,27 @@ __device__ __forceinline__ uint32_t pack2(float x, float y) {
   else return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
+// How the scheduler is to place a run of kReads reads of LDS and the kPer products that each feeds: kAhead reads first, then a read behind every kPer products.  Left
+// to itself it reads two pieces, waits for both and multiplies: a trip to LDS (over 100 cycles) for every 64 cycles of products.
+template <int kReads, int kPer, int kAhead>
+__device__ __forceinline__ void reads_ahead() {
+  constexpr int kProducts = 0x008, kLdsReads = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kLdsReads, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < kReads - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(kProducts, kPer, 0);
+    __builtin_amdgcn_sched_group_barrier(kLdsReads, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(kProducts, kAhead * kPer, 0);
+}
+
+// sum + the two values of a pair.
+template <class Elt>
+__device__ __forceinline__ float add_pair(uint32_t pair, float sum) {
+  if constexpr (std::is_same<Elt, F16>::value) return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), f16x2{(_Float16)1.f, (_Float16)1.f}, sum, false);
+  else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3f803f80u), sum, false);
+}
+
 template <class Elt, int D>
 __global__ __launch_bounds__(kPromptThreads)
 __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a) {
@@ -114,6 +135,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   constexpr int ROWB = Shape::kRowBytes, kKRow = Shape::kKRow, kVRow = Shape::kVRow;
   constexpr int kLanes = ROWB / 16;               // lanes of a row in a load of K
   constexpr int kBlocks = D / 32;
+  constexpr int kAhead = 4;                       // pieces read from LDS ahead of the products they feed
   constexpr int kUnit = kHalf ? D / 16 : 4;       // 16 bits: dimensions of V that a lane transposes (of 4 positions)
 
   __shared__ __attribute__((aligned(16))) unsigned char s_k[2][Shape::kKBytes];
@@ -173,10 +195,16 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   // ---- the cache's rows: global memory -> registers -> LDS -------------------------------------------------
   u32x4 kx[NL], vx[NL];
   uint32_t outside;
-  auto fetch = [&](int p0) {
-    const int p = p0 + wave * RW;  // the wave's rows of the tile lie in one page
+  int pages = -1;  // lane l: the page of the wave's rows of tile 64 k + l, k the last that was looked up
+  auto look_up = [&](int i) {
+    const int entry = (tile_pos(min(i + lane, last_tile - 1)) + wave * RW) >> a.page_shift;
+    pages = entry < a.table_pages ? table[entry] : -1;
+  };
+  auto fetch = [&](int i) {
+    const int p = tile_pos(i) + wave * RW;  // the wave's rows of the tile lie in one page
     const int entry = p >> a.page_shift, in_page = p & ((1 << a.page_shift) - 1);
-    const int page = entry < a.table_pages ? __builtin_amdgcn_readfirstlane(table[entry]) : -1;
+    if ((i - first_tile) % 64 == 0) look_up(i);
+    const int page = __builtin_amdgcn_readlane(pages, (i - first_tile) % 64);
     const bool good = (uint32_t)page < (uint32_t)a.num_pages;
     outside = !good && p < high ? 1u : 0u;
     const int there = good ? clampi(t.len - (entry << a.page_shift), 0, 1 << a.page_shift) : 0;  // rows of the page that are the sequence's
@@ -239,7 +267,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
         const int d = kUnit * (lane & 15) + j;
         const uint32_t sel = (j & 1) ? 0x07060302u : 0x05040100u;
         const u32x2 w = {__builtin_amdgcn_perm(x[1][j / 2], x[0][j / 2], sel), __builtin_amdgcn_perm(x[3][j / 2], x[2][j / 2], sel)};
-        *reinterpret_cast<u32x2*>(&s_v[buf][d * kVRow + 16 * (piece ^ ((d >> 3) & 7)) + within]) = w;
+        *reinterpret_cast<u32x2*>(&s_v[buf][d * kVRow + 16 * (piece ^ ((d >> 4) & 7)) + within]) = w;
       }
     } else {
 #pragma unroll
@@ -260,34 +288,38 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     }
   };
 
+  constexpr float kLargeShift = 4194304.f;  // 2^22: a rounding of a quarter at most
+  float shift = kShift;
+  bool large = false;
   float ref = -INFINITY, lsum = 0.f;  // reference of the weights: the largest unscaled score; this lane's share of their sum
   f32x16 O[kBlocks];
   auto sees = [&](int p) { return p <= at && (a.window == 0 || p > at - a.window || p < a.sinks); };
 
+  const int v_lane = col * kVRow + 16 * (half ^ (col >> 4));
   auto compute = [&](int buf, int p0, auto checked) {
     constexpr bool kChecked = decltype(checked)::value;
     if (!wave_works || p0 > wave_last) return;
     if (a.window > 0 && p0 + KT - 1 <= wave_first - a.window && p0 >= a.sinks) return;
+    constexpr f32x16 kZero = {};
     f32x16 S[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) S[n][r] = 0.f;
       const unsigned char* kr = &s_k[buf][(32 * n + col) * kKRow + 16 * half];
 #pragma unroll
       for (int mm = 0; mm < NP; ++mm) {
         const u32x4 km = *reinterpret_cast<const u32x4*>(kr + 32 * mm);
         if constexpr (kHalf) {
-          S[n] = mfma32<Elt>(km, qr[mm], S[n]);
+          S[n] = mfma32<Elt>(km, qr[mm], mm == 0 ? kZero : S[n]);
         } else {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const uint32_t kw = km[k], qw = qr[mm][k];
-            S[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, kw), __builtin_bit_cast(float, qw), S[n], 0, 0, 0);
+            S[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, kw), __builtin_bit_cast(float, qw), mm == 0 && k == 0 ? kZero : S[n], 0, 0, 0);
           }
         }
       }
     }
+    reads_ahead<NB * NP, kHalf ? 1 : 4, kAhead>();
     const uint32_t out_bits = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[buf]);
     const bool whole = p0 + KT - 1 <= wave_first && (a.window == 0 || p0 > wave_last - a.window || p0 + KT <= a.sinks) && out_bits == 0;
     if (!whole) {
@@ -315,43 +347,59 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
       lsum *= alpha;
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e) O[e] *= alpha;
+      shift = kShift - safe * post;
+      large = __builtin_amdgcn_ballot_w64(!(fabsf(shift) < kLargeShift)) != 0;
     }
-    const float safe = ref == -INFINITY ? 0.f : ref;
+    // A weight is exp2(score * post + shift), shift = -reference * post rounded: its rounding is a factor of all weights and goes out with their sum.
+    // Where it is no longer small the difference from the reference is taken first, which is exact.
+    if (__builtin_expect(large, 0)) {
+      const float safe = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < NB; ++n) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        S[n][r] = __builtin_amdgcn_exp2f(fmaf(S[n][r] - safe, post, kShift));
-        sum[r & 3] += S[n][r];
+        for (int r = 0; r < 16; ++r) S[n][r] = __builtin_amdgcn_exp2f(fmaf(S[n][r] - safe, post, kShift));
       }
-      lsum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    } else {
+#pragma unroll
+      for (int n = 0; n < NB; ++n) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[n][r] = __builtin_amdgcn_exp2f(fmaf(S[n][r], post, shift));
+      }
     }
     if constexpr (kHalf) {
       u32x4 P[NB][2];
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of the weights as they are rounded
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) P[n][c][k] = pack2<Elt>(S[n][8 * c + 2 * k], S[n][8 * c + 2 * k + 1]);
+          for (int k = 0; k < 4; ++k) {
+            P[n][c][k] = pack2<Elt>(S[n][8 * c + 2 * k], S[n][8 * c + 2 * k + 1]);
+            sum[k] = add_pair<Elt>(P[n][c][k], sum[k]);
+          }
         }
       }
+      lsum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      const unsigned char* vr = &s_v[buf][0] + v_lane;
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e) {
-        const int d = 32 * e + col;
-        const unsigned char* vr = &s_v[buf][d * kVRow];
-        const int turn = (d >> 3) & 7;
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
-            const u32x4 vm = *reinterpret_cast<const u32x4*>(vr + 16 * ((4 * n + 2 * c + half) ^ turn));
+            // piece 4 n + 2 c + half of dimension 32 e + col, at its place: bit 0 of the turn is the lane's, the others are e's
+            const u32x4 vm = *reinterpret_cast<const u32x4*>(vr + 32 * e * kVRow + 16 * ((4 * n + 2 * c) ^ (2 * e)));
             O[e] = mfma32<Elt>(vm, P[n][c], O[e]);
           }
         }
       }
+      reads_ahead<kBlocks * NB * 2, 1, kAhead>();
     } else {
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[r & 3] += S[0][r];
+      lsum += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e) {
 #pragma unroll
@@ -405,6 +453,8 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     constexpr bool kChecked = decltype(checked)::value;
     ref = -INFINITY;
     lsum = 0.f;
+    shift = kShift;
+    large = false;
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e) {
 #pragma unroll
@@ -415,18 +465,18 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
       if (tid < 4) s_wild[tid >> 1][tid & 1] = 0u;
       __syncthreads();
     }
-    fetch(tile_pos(first_tile));
+    fetch(first_tile);
     lay_down(0, checked);
     __syncthreads();
     int buf = 0;
     for (int i = first_tile; i < last_tile; ++i) {
-      if (i + 1 < last_tile) fetch(tile_pos(i + 1));
+      fetch(min(i + 1, last_tile - 1));  // (the last tile a second time rather than a branch, which would cost copies of all these registers)
       compute(buf, tile_pos(i), checked);
       if (kChecked) {
         __syncthreads();
         if (tid < 2) s_wild[buf][tid] = 0u;  // (for the tile after next)
       }
-      if (i + 1 < last_tile) lay_down(buf ^ 1, checked);
+      lay_down(buf ^ 1, checked);
       __syncthreads();
       buf ^= 1;
     }
@@ -459,7 +509,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     return;
   }
   // The wave's rows through LDS, so that they are stored whole (its own part of the first half, which nobody reads any more).
-  const float sum = lsum != 0.f ? lsum : 1.f;
+  const float inv = 1.f / (lsum != 0.f ? lsum : 1.f);
   static_assert(32 * kPromptWaves * kKRow <= 2 * Shape::kKBytes || kHalf == false, "the tile's outputs fit");
   if constexpr (kHalf) {
     unsigned char* mine = &s_k[0][0] + wave * 32 * kKRow;
@@ -467,7 +517,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     for (int e = 0; e < kBlocks; ++e) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const u32x2 w = {pack2<Elt>(O[e][4 * g] / sum, O[e][4 * g + 1] / sum), pack2<Elt>(O[e][4 * g + 2] / sum, O[e][4 * g + 3] / sum)};
+        const u32x2 w = {pack2<Elt>(O[e][4 * g] * inv, O[e][4 * g + 1] * inv), pack2<Elt>(O[e][4 * g + 2] * inv, O[e][4 * g + 3] * inv)};
         *reinterpret_cast<u32x2*>(mine + col * kKRow + 2 * (32 * e + 8 * g + 4 * half)) = w;
       }
     }
@@ -485,7 +535,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     for (int e = 0; e < kBlocks; ++e) {
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(out + 32 * e + 8 * g) = f32x4{O[e][4 * g] / sum, O[e][4 * g + 1] / sum, O[e][4 * g + 2] / sum, O[e][4 * g + 3] / sum};
+        *reinterpret_cast<f32x4*>(out + 32 * e + 8 * g) = f32x4{O[e][4 * g] * inv, O[e][4 * g + 1] * inv, O[e][4 * g + 2] * inv, O[e][4 * g + 3] * inv};
     }
   }
 }
