@@ -51,11 +51,11 @@ typedef struct span_paged_desc {
   const int64_t* tokens_per_seq; /* paged_span_decode_attn: HOST int64 [batch] or NULL: attended positions of every
                               sequence as span_validate returns them; they only set the slices (a wrong number costs
                               time, not correctness).  Read during the call only.                           */
-  void* workspace;         /* device, 256-byte aligned, at least paged_workspace_bytes(); for one-token calls its
-                              ticket counters (the first 4 * batch * kv_heads bytes, rounded up to 256) must be zero
-                              before the first call (paged_workspace_init); every call leaves them zero again.  A
-                              workspace that served another batch, another number of KV heads or paged_evict is
-                              initialised again.  Two calls that may overlap in time must not share one.    */
+  void* workspace;         /* device, 256-byte aligned, at least paged_workspace_bytes(); for one-token calls and
+                              paged_evict its ticket counters (the first 4 * batch * (kv_heads + 1) bytes, rounded up to
+                              256) must be zero before the first call (paged_workspace_init); every call leaves them
+                              zero again.  A workspace that served another batch, another number of KV heads or
+                              paged_prompt_attn is initialised again.  Two calls that may overlap in time must not share one.    */
   size_t workspace_bytes;
   void* stream;            /* hipStream_t; NULL = the default stream                                        */
 } span_paged_desc_t;

@@ -94,28 +94,76 @@ struct EvictArgs {
   float* weights_out;
   int32_t* positions_out;
   int32_t* new_lens;
-  int32_t* moves;  // per (sequence, KV head): count, 0, `most` pairs of slots, to and from
-  int32_t kv_heads, table_pages, page_shift, num_pages, max_len, budget, sinks, recent, most;
+  uint32_t* counters;  // tickets: of every (sequence, KV head), then of every sequence; zero between calls
+  int32_t* moves;      // per (sequence, KV head): count, 0, `most` pairs of slots, to and from
+  int32_t kv_heads, table_pages, page_shift, num_pages, max_len, budget, sinks, recent, most, row_shift, in_place;
 };
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kHoleList = 4096;  // free slots whose list fits LDS
 
+// A pair's rows that move, pair_of(m) = (to, from) for m < count, by `threads` threads.  Slots from the budget on are only read, slots below it that fell
+// free only written, so the order does not matter.
+template <class PairOf>
+static __device__ __forceinline__ void move_rows(const EvictArgs& a, int bh, int thread, int threads, int count, PairOf&& pair_of) {
+  const int b = bh / a.kv_heads, h = bh % a.kv_heads;
+  const int32_t* table = a.block_table + (size_t)b * a.table_pages;
+  const int piece = thread & ((1 << a.row_shift) - 1), rows = threads >> a.row_shift;
+  auto place = [&](int x) {
+    const size_t page = (size_t)(x >> a.page_shift), in_page = (size_t)(x & ((1 << a.page_shift) - 1));
+    return (((((page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) + in_page)) << a.row_shift) + (size_t)piece;
+  };
+  constexpr int kAhead = 2;  // rows of a thread on their way
+  for (int m0 = thread >> a.row_shift; m0 < count; m0 += kAhead * rows) {
+    int to[kAhead], from[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int m = m0 + k * rows;
+      const i32x2 pair = pair_of(min(m, count - 1));
+      to[k] = pool_row(table, pair[0], a.page_shift, a.num_pages);
+      from[k] = pool_row(table, pair[1], a.page_shift, a.num_pages);
+      if (m >= count || from[k] < 0) to[k] = -1;
+    }
+    u32x4 kx[kAhead], vx[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      kx[k] = __builtin_nontemporal_load(a.k + place(max(from[k], 0)));  // (some row of the pool rather than a branch)
+      vx[k] = __builtin_nontemporal_load(a.v + place(max(from[k], 0)));
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (to[k] >= 0) {
+        a.k[place(to[k])] = kx[k];
+        a.v[place(to[k])] = vx[k];
+      }
+    }
+  }
+}
+
 // Which rows stay, one workgroup per (sequence, KV head).  Every slot has a 32-bit key that orders as it is to be kept: largest for the protected ones, then the
-// weight's bits made monotone; equal keys by slot.  The budget-th largest key is found digit by digit (11, 11 and 10 bits) with histograms in LDS; the
+// weight's bits made monotone, 1 for NaN, 0 for no slot; equal keys by slot.  The budget-th largest key is found digit by digit (11, 11 and 10 bits) with histograms in LDS; the
 // first digit holds a weight's exponent and two bits of its mantissa, so that even weights of one size spread over some bins, and the protected ones, which
 // all meet, are counted apart.  Then the waves, each with its own run of slots, count equal keys, free slots and rows to move in order.
-// kKeys: slots of a thread, whose keys stay in registers; 0: any number, keys made again from the weights each time.  us, 16 x 8 caches of ~4350 slots
-// and 5 x 16 of ~6500, with keys in LDS and two bits a step by ballots (16 rounds) -> so: 30.5 and 62.9 -> 12.6 and 19.8.
+// kKeys: slots of a thread, whose keys stay in registers; 0: any number, keys made again from the weights each time.
+// With keys in registers the workgroup also moves rows: where the card has more CUs than there are pairs, each pair has several workgroups that find the
+// same selection and move a part of the rows each, so nothing waits for a second launch.  Longer caches leave the list in the workspace, for move_kernel.
+// What bounds it: the passes over a CU's slots are bound by instructions (some 15 a piece of 64 slots in each of seven passes), the moves by memory.
+// us of a call, 16 x 8 caches of ~4350 slots down to 4096 and 5 x 16 of 900 .. 12000 down to 2048: keys in LDS and two bits a step by ballots, and a second
+// launch that moves: 40 and 75; histograms of three digits, keys in registers: 23.3 and 32.3; one launch, fewer instructions a piece: 18.0 and 27.5.
+// (With outputs in place, whose writers are found by tickets, a call of few rows takes about 1 us more.)
 template <int kKeys>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs a) {
+  constexpr bool kMoves = kKeys > 0;
   __shared__ int s_bins[2048];
-  __shared__ int s_holes[kHoleList];
-  __shared__ int s_wave[4][kSelectWaves];
-  __shared__ int s_pick[2];
+  __shared__ int s_holes[kMoves ? 1 : kHoleList];
+  __shared__ uint16_t s_pairs[kMoves ? kKeys * kSelectThreads / 2 : 1][2];  // to and from (half of the slots at most: one falls free for each that moves)
+  __shared__ int s_wave[6][kSelectWaves];  // (a row of its own for all that no barrier parts)
+  __shared__ int s_pick[3];
+  __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.x, b = bh / a.kv_heads;
   const int n = clampi(a.ctx_lens[b], 0, a.max_len), keep = a.budget;
+  const int part = kMoves ? (int)blockIdx.y : 0, parts = kMoves ? (int)gridDim.y : 1;
   const size_t row = (size_t)bh * (size_t)a.max_len;
   const float* weights = a.weights + row;
   const int32_t* positions = a.positions != nullptr ? a.positions + row : nullptr;
@@ -123,8 +171,9 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
   int32_t* positions_out = a.positions_out != nullptr ? a.positions_out + row : nullptr;
   int32_t* moves = a.moves + (size_t)bh * (size_t)(2 + 2 * a.most);
   if (n <= keep) {
-    if (tid == 0) moves[0] = 0;
-    for (int i = tid; i < n; i += kSelectThreads) {
+    if (kMoves && bh % a.kv_heads == 0 && part == 0 && tid == 0) a.new_lens[b] = n;  // (which is what others may still read there)
+    if (!kMoves && tid == 0) moves[0] = 0;
+    for (int i = part * kSelectThreads + tid; i < n; i += parts * kSelectThreads) {
       weights_out[i] = weights[i];
       if (positions_out != nullptr) positions_out[i] = positions[i];
     }
@@ -167,23 +216,27 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
     last = __builtin_amdgcn_readlane(wave_inclusive_max(last), 63);
     if (lane == 0) s_wave[3][wave] = last;
   }
-  s_bins[tid] = s_bins[tid + kSelectThreads] = 0;
+  i32x2& bins = *reinterpret_cast<i32x2*>(&s_bins[2 * tid]);
+  bins = i32x2{0, 0};
   __syncthreads();
   auto over_waves = [&](int which) { return lane < kSelectWaves ? s_wave[which][lane] : 0; };  // (summed or scanned by every wave for itself)
   if (positions != nullptr) last = __builtin_amdgcn_readlane(wave_inclusive_max(over_waves(3)), 63);
   auto key_of = [&](int p, uint32_t u) -> uint32_t {
     if (p < a.sinks || last - p < a.recent) return 0xffffffffu;
-    if ((u & 0x7fffffffu) > 0x7f800000u) return 0u;  // NaN
+    if ((u & 0x7fffffffu) > 0x7f800000u) return 1u;  // NaN
     if (u == 0x80000000u) return 0x80000000u;        // -0 is 0
     return u ^ ((u >> 31) != 0 ? 0xffffffffu : 0x80000000u);
   };
   if constexpr (kKeys > 0) {
 #pragma unroll
-    for (int j = 0; j < kKeys; ++j) held[j] = key_of(positions != nullptr ? position[j] : begin + 64 * j + lane, __builtin_bit_cast(uint32_t, weight[j]));
+    for (int j = 0; j < kKeys; ++j) {
+      const int i = begin + 64 * j + lane;
+      held[j] = i < end ? key_of(positions != nullptr ? position[j] : i, __builtin_bit_cast(uint32_t, weight[j])) : 0u;
+    }
   }
   auto key = [&](int j, int i) -> uint32_t {
     if constexpr (kKeys > 0) return held[j];
-    else return i < n ? key_of(positions != nullptr ? positions[i] : i, __builtin_bit_cast(uint32_t, weights[i])) : 0u;
+    else return i < end ? key_of(positions != nullptr ? positions[i] : i, __builtin_bit_cast(uint32_t, weights[i])) : 0u;
   };
   auto count_if = [&](bool x) { return (int)__popcll(__builtin_amdgcn_ballot_w64(x)); };
   auto lanes_below = [&](uint64_t who) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u)); };
@@ -191,14 +244,22 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
   int safe = 0;
   pieces([&](int j, int i) {
     const uint32_t x = key(j, i);
-    safe += count_if(i < end && x == 0xffffffffu);
-    if (i < end && x != 0xffffffffu) atomicAdd(&s_bins[2047 - (x >> 21)], 1);
+    safe += count_if(x == 0xffffffffu);
+    if (x != 0xffffffffu) atomicAdd(&s_bins[2047 - (int)(x >> 21)], 1);
   });
   if (lane == 0) s_wave[0][wave] = safe;
   __syncthreads();
+  // All of the workgroup's threads hold their weights and positions now.  Where outputs are inputs, the last of a pair's workgroups to come here writes all of
+  // the pair's, and the last of a sequence's the length.  (Nothing that others write is read after it, and these reads are done: no ordering is needed.)
+  uint32_t ticket = 0, sequence_ticket = 0;
+  if (kMoves && a.in_place != 0 && tid == 0) {
+    if (parts > 1) ticket = __hip_atomic_fetch_add(a.counters + bh, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    sequence_ticket = __hip_atomic_fetch_add(a.counters + gridDim.x + b, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   safe = __builtin_amdgcn_readlane(wave_inclusive_scan(over_waves(0)), 63);
   uint32_t at = 0xffffffffu;  // the key of the last row that stays
   int ties = keep;            // of the slots with that key so many stay, the first
+  int tied_slots = safe;      // the slots with that key
   if (safe < keep) {
     ties = keep - safe;
     at = 0;
@@ -209,88 +270,131 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
         const int above = digit == 1 ? 21 : 10, mask = digit == 1 ? 2047 : 1023;
         pieces([&](int j, int i) {
           const uint32_t x = key(j, i);
-          if (i < end && x != 0xffffffffu && x >> above == at >> above) atomicAdd(&s_bins[mask - (int)(x >> shift & (uint32_t)mask)], 1);
+          if (x != 0xffffffffu && (x ^ at) >> above == 0) atomicAdd(&s_bins[mask - (int)(x >> shift & (uint32_t)mask)], 1);
         });
         __syncthreads();
       }
-      const int c0 = s_bins[2 * tid], c1 = s_bins[2 * tid + 1];
+      const int c0 = bins[0], c1 = bins[1];
       const int incl = wave_inclusive_scan(c0 + c1);
       if (lane == 63) s_wave[1][wave] = incl;
       __syncthreads();
-      s_bins[2 * tid] = s_bins[2 * tid + 1] = 0;
+      bins = i32x2{0, 0};
       const int waves_incl = wave_inclusive_scan(over_waves(1));
       const int before = incl - c0 - c1 + (wave > 0 ? __builtin_amdgcn_readlane(waves_incl, wave - 1) : 0);
       if (before < ties && before + c0 + c1 >= ties) {
         const bool first = before + c0 >= ties;
         s_pick[0] = 2 * tid + (first ? 0 : 1);
         s_pick[1] = before + (first ? 0 : c0);
+        s_pick[2] = first ? c0 : c1;
       }
       __syncthreads();
       at |= (uint32_t)((digit == 2 ? 1023 : 2047) - s_pick[0]) << shift;
       ties -= s_pick[1];
+      tied_slots = s_pick[2];
     }
   }
 
-  int equal = 0;
-  pieces([&](int j, int i) { equal += count_if(i < end && key(j, i) == at); });
-  if (lane == 0) s_wave[2][wave] = equal;
-  __syncthreads();
   auto before_wave = [&](int which) {
     const int incl = wave_inclusive_scan(over_waves(which));
     return wave > 0 ? __builtin_amdgcn_readlane(incl, wave - 1) : 0;
   };
-  const int ties_before = before_wave(2);
+  const bool all_tied = ties == tied_slots;  // (the common case: weights differ)
+  int ties_before = 0;
+  if (!all_tied) {
+    int equal = 0;
+    pieces([&](int j, int i) { equal += count_if(key(j, i) == at); });
+    if (lane == 0) s_wave[2][wave] = equal;
+    __syncthreads();
+    ties_before = before_wave(2);
+  }
   int tied = ties_before;
-  auto stays = [&](int j, int i) {  // called piece by piece
+  auto who_stays = [&](int j, int i) -> uint64_t {  // called piece by piece
     const uint32_t x = key(j, i);
-    const uint64_t eq = __builtin_amdgcn_ballot_w64(i < end && x == at);
-    const bool yes = i < end && (x > at || (x == at && tied + lanes_below(eq) < ties));
+    if (all_tied) return __builtin_amdgcn_ballot_w64(x >= at);
+    const uint64_t eq = __builtin_amdgcn_ballot_w64(x == at);
+    const bool yes = x > at || (x == at && tied + lanes_below(eq) < ties);
     tied += __popcll(eq);
-    return yes;
+    return __builtin_amdgcn_ballot_w64(yes);
   };
+  // of a piece: the slots below the budget that fall free, the rows beyond it that stay
+  const int below = min(end, keep);
+  auto free_slots = [&](uint64_t stay, int i) { return ~stay & __builtin_amdgcn_ballot_w64(i < below); };
+  auto moving = [&](uint64_t stay, int i) { return stay & __builtin_amdgcn_ballot_w64(i >= keep); };
   int holes = 0, movers = 0;
   uint64_t staying[kHeld];  // registers: found once
   pieces([&](int j, int i) {
-    const bool yes = stays(j, i);
-    if constexpr (kKeys > 0) staying[j] = __builtin_amdgcn_ballot_w64(yes);
-    holes += count_if(!yes && i < min(end, keep));
-    movers += count_if(yes && i >= keep);
+    const uint64_t stay = who_stays(j, i);
+    if constexpr (kKeys > 0) staying[j] = stay;
+    holes += __popcll(free_slots(stay, i));
+    movers += __popcll(moving(stay, i));
   });
   if (lane == 0) {
-    s_wave[0][wave] = holes;
-    s_wave[1][wave] = movers;
+    s_wave[4][wave] = holes;
+    s_wave[5][wave] = movers;
   }
+  if (kMoves && tid == 0) s_last = ticket == (uint32_t)(parts - 1) ? 1 : 0;
   __syncthreads();
-  holes = before_wave(0);
-  movers = before_wave(1);
-  const int count = __builtin_amdgcn_readlane(wave_inclusive_scan(over_waves(1)), 63);
-  if (tid == 0) moves[0] = count;
+  holes = before_wave(4);
+  movers = before_wave(5);
+  const int num_moves = __builtin_amdgcn_readlane(wave_inclusive_scan(over_waves(5)), 63);
   // The free slots are listed; then who moves reads its slot, writes the pair down and its weight and position there.  Every slot's own weight and
   // position are read by its own thread only, ahead of what it writes, so the outputs may be the arrays themselves: a free slot's are not needed.
-  const bool in_lds = count <= kHoleList;
+  const bool in_lds = kMoves || num_moves <= kHoleList;
   tied = ties_before;
-  int at_hole = holes;
+  int at_hole = holes, at_mover = movers;
   pieces([&](int j, int i) {
-    bool yes;
-    if constexpr (kKeys > 0) yes = staying[j] >> lane & 1u;
-    else yes = stays(j, i);
-    const bool hole = !yes && i < min(end, keep);
-    const uint64_t who = __builtin_amdgcn_ballot_w64(hole);
-    const int m = at_hole + lanes_below(who);
-    if (hole) (in_lds ? s_holes[m] : moves[2 + 2 * m]) = i;
-    at_hole += __popcll(who);
+    uint64_t stay;
+    if constexpr (kKeys > 0) stay = staying[j];
+    else stay = who_stays(j, i);
+    const uint64_t who = free_slots(stay, i);
+    if (who != 0) {
+      const int m = at_hole + lanes_below(who);
+      if (who >> lane & 1u) {
+        if constexpr (kMoves) s_pairs[m][0] = (uint16_t)i;
+        else (in_lds ? s_holes[m] : moves[2 + 2 * m]) = i;
+      }
+      at_hole += __popcll(who);
+    }
+    if constexpr (kMoves) {
+      const uint64_t from = moving(stay, i);
+      if (from != 0) {
+        if (from >> lane & 1u) s_pairs[at_mover + lanes_below(from)][1] = (uint16_t)i;
+        at_mover += __popcll(from);
+      }
+    }
   });
   __syncthreads();
+  if constexpr (kMoves) {
+    move_rows(a, bh, part * kSelectThreads + tid, parts * kSelectThreads, num_moves, [&](int m) {
+      const uint32_t pair = *reinterpret_cast<const uint32_t*>(s_pairs[m]);
+      return i32x2{(int)(pair & 0xffffu), (int)(pair >> 16)};
+    });
+    if (tid == 0) {
+      if (a.in_place == 0) {
+        if (bh % a.kv_heads == 0 && part == 0) a.new_lens[b] = keep;
+      } else if (sequence_ticket == (uint32_t)(a.kv_heads * parts - 1)) {
+        __hip_atomic_store(a.counters + gridDim.x + b, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        a.new_lens[b] = keep;
+      }
+    }
+    if (a.in_place != 0 && parts > 1) {
+      if (s_last == 0) return;
+      if (tid == 0) __hip_atomic_store(a.counters + bh, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  } else if (tid == 0) {
+    moves[0] = num_moves;
+  }
   tied = ties_before;
-  int at_mover = movers;
+  at_mover = movers;
   pieces([&](int j, int i) {
-    bool yes;
-    if constexpr (kKeys > 0) yes = staying[j] >> lane & 1u;
-    else yes = stays(j, i);
-    const bool mover = yes && i >= keep;
-    const uint64_t who = __builtin_amdgcn_ballot_w64(mover);
+    uint64_t stay;
+    if constexpr (kKeys > 0) stay = staying[j];
+    else stay = who_stays(j, i);
+    const uint64_t who = moving(stay, i);
     const int m = at_mover + lanes_below(who);
     at_mover += __popcll(who);
+    if (kMoves && a.in_place == 0 && (uint32_t)(i - lane) / 64u % (uint32_t)parts != (uint32_t)part) return;  // (another workgroup's)
+    const bool yes = stay >> lane & 1u, mover = who >> lane & 1u;
     if (i < end) {
       float w = 0.f;
       int p = -1;
@@ -304,8 +408,13 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
         }
       }
       if (mover) {
-        const int to = in_lds ? s_holes[m] : moves[2 + 2 * m];
-        *reinterpret_cast<i32x2*>(moves + 2 + 2 * m) = i32x2{to, i};
+        int to;
+        if constexpr (kMoves) {
+          to = s_pairs[m][0];
+        } else {
+          to = in_lds ? s_holes[m] : moves[2 + 2 * m];
+          *reinterpret_cast<i32x2*>(moves + 2 + 2 * m) = i32x2{to, i};
+        }
         if (kKeys > 0) {
           weights_out[to] = w;
           if (positions_out != nullptr) positions_out[to] = p;
@@ -322,7 +431,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
   if constexpr (kKeys == 0) {
     // (keys were made from the arrays up to here: what changes a weight or a position that a key is made from comes after them all)
     __syncthreads();
-    for (int m = tid; m < count; m += kSelectThreads) {
+    for (int m = tid; m < num_moves; m += kSelectThreads) {
       const int to = moves[2 + 2 * m], from = moves[3 + 2 * m];
       weights_out[to] = weights[from];
       if (positions_out != nullptr) positions_out[to] = positions[from];
@@ -335,31 +444,20 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const EvictArgs 
   }
 }
 
-// The rows that move: slots from the budget on are only read, slots below it that fell free only written.
-template <int kRowBytes>
+// The rows that move, of lists that select_kernel left in the workspace.
 __global__ __launch_bounds__(256) void move_kernel(const EvictArgs a) {
-  constexpr int kLanes = kRowBytes / 16, kRows = 256 / kLanes;  // lanes of a row, rows of a workgroup at a time
-  const int bh = blockIdx.x, b = bh / a.kv_heads, h = bh % a.kv_heads;
+  const int bh = blockIdx.x, b = bh / a.kv_heads;
   const int32_t* moves = a.moves + (size_t)bh * (size_t)(2 + 2 * a.most);
-  const int32_t* table = a.block_table + (size_t)b * a.table_pages;
-  if (h == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.new_lens[b] = min(clampi(a.ctx_lens[b], 0, a.max_len), a.budget);
-  const int count = moves[0], piece = (int)threadIdx.x % kLanes;
-  auto place = [&](int x) {
-    const size_t page = (size_t)(x >> a.page_shift), in_page = (size_t)(x & ((1 << a.page_shift) - 1));
-    return (((page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) + in_page) * (size_t)kLanes + (size_t)piece;
-  };
-  for (int m = (int)blockIdx.y * kRows + (int)threadIdx.x / kLanes; m < count; m += (int)gridDim.y * kRows) {
-    const i32x2 pair = *reinterpret_cast<const i32x2*>(moves + 2 + 2 * m);
-    const int to = pool_row(table, pair[0], a.page_shift, a.num_pages), from = pool_row(table, pair[1], a.page_shift, a.num_pages);
-    if (to < 0 || from < 0) continue;
-    const size_t src = place(from), dst = place(to);
-    const u32x4 kx = __builtin_nontemporal_load(a.k + src), vx = __builtin_nontemporal_load(a.v + src);
-    a.k[dst] = kx;
-    a.v[dst] = vx;
-  }
+  if (bh % a.kv_heads == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.new_lens[b] = min(clampi(a.ctx_lens[b], 0, a.max_len), a.budget);
+  move_rows(a, bh, (int)(blockIdx.y * 256 + threadIdx.x), (int)gridDim.y * 256, moves[0],
+            [&](int m) { return *reinterpret_cast<const i32x2*>(moves + 2 + 2 * m); });
 }
 
 constexpr int64_t kMoveWorkgroups = 2048;
+// A pair gets several workgroups while there are CUs for them and rows for one pass of each.  The batch of 16 x 8 caches above takes 20 us with 256 workgroups
+// and 30 with 512, whose second halves select once more when the first are done; rows for one, two and four passes: 12.3, 13.8 and 17.8 us for 2 x 32 caches of
+// 1700 slots.
+constexpr unsigned kSelectWorkgroups = 256;
 
 }  // namespace
 }  // namespace spanattn
@@ -417,7 +515,8 @@ extern "C" int paged_evict(const span_paged_desc_t* desc, void* k_pages, void* v
   a.weights_out = weights_out;
   a.positions_out = positions_out;
   a.new_lens = new_lens;
-  a.moves = (int32_t*)desc->workspace;
+  a.counters = (uint32_t*)desc->workspace;
+  a.moves = (int32_t*)((char*)desc->workspace + counter_bytes(desc));
   a.kv_heads = desc->kv_heads;
   a.table_pages = desc->table_pages;
   a.page_shift = page_shift(desc);
@@ -426,25 +525,37 @@ extern "C" int paged_evict(const span_paged_desc_t* desc, void* k_pages, void* v
   a.budget = desc->budget;
   a.sinks = desc->sinks;
   a.recent = desc->recent;
-  a.most = a.max_len > a.budget ? (a.max_len - a.budget < a.budget ? a.max_len - a.budget : a.budget) : 0;
+  a.most = most_moves(desc);
   const unsigned pairs = (unsigned)desc->batch * (unsigned)desc->kv_heads;
+  const int row_bytes = desc->head_dim * (desc->dtype == SPAN_F32 ? 4 : 2);
+  a.row_shift = 31 - __builtin_clz((unsigned)row_bytes / 16u);
   hipStream_t stream = (hipStream_t)desc->stream;
-  auto select = [&](auto keys) { hipLaunchKernelGGL(select_kernel<decltype(keys)::value>, dim3(pairs), dim3(kSelectThreads), 0, stream, a); };
+  const unsigned passes = (unsigned)a.most / (unsigned)(kSelectThreads >> a.row_shift);
+  const unsigned parts = std::max(std::min(kSelectWorkgroups / pairs, passes), 1u);
+  const size_t slots = (size_t)pairs * (size_t)a.max_len * 4, lens = (size_t)desc->batch * 4;
+  auto meet = [](const void* x, size_t x_bytes, const void* y, size_t y_bytes) {
+    return x != nullptr && y != nullptr && (uintptr_t)x < (uintptr_t)y + y_bytes && (uintptr_t)y < (uintptr_t)x + x_bytes;
+  };
+  a.in_place = meet(ctx_lens, lens, new_lens, lens);
+  for (const void* x : {(const void*)weights, (const void*)positions}) {
+    for (const void* y : {(const void*)weights_out, (const void*)positions_out}) a.in_place |= meet(x, slots, y, slots);
+  }
+  auto select = [&](auto keys) {
+    constexpr int kKeys = decltype(keys)::value;
+    hipLaunchKernelGGL(select_kernel<kKeys>, dim3(pairs, kKeys > 0 ? parts : 1), dim3(kSelectThreads), 0, stream, a);
+  };
   if (a.max_len <= 2 * kSelectThreads) select(std::integral_constant<int, 2>{});
   else if (a.max_len <= 8 * kSelectThreads) select(std::integral_constant<int, 8>{});
   else if (a.max_len <= 16 * kSelectThreads) select(std::integral_constant<int, 16>{});
-  else if (a.max_len <= 32 * kSelectThreads) select(std::integral_constant<int, 32>{});
+  else if (a.max_len <= kMostKeysHeld) select(std::integral_constant<int, 32>{});
   else select(std::integral_constant<int, 0>{});
   const int src = launched();
-  if (src != SPAN_OK) return src;
-  const int row_bytes = desc->head_dim * (desc->dtype == SPAN_F32 ? 4 : 2), rows = 256 / (row_bytes / 16);
+  if (src != SPAN_OK || a.max_len <= kMostKeysHeld) return src;
+  const int rows = 256 >> a.row_shift;
   int64_t splits = (kMoveWorkgroups + pairs - 1) / pairs;
   const int64_t useful = (a.most + rows - 1) / rows;
   if (splits > useful) splits = useful;
   if (splits < 1) splits = 1;
-  const dim3 grid(pairs, (unsigned)splits);
-  if (row_bytes == 128) hipLaunchKernelGGL(move_kernel<128>, grid, dim3(256), 0, stream, a);
-  else if (row_bytes == 256) hipLaunchKernelGGL(move_kernel<256>, grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL(move_kernel<512>, grid, dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(move_kernel, dim3(pairs, (unsigned)splits), dim3(256), 0, stream, a);
   return launched();
 }

@@ -688,7 +688,6 @@ __global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* p, size_t n)
   if (i < n) p[i] = 0u;
 }
 
-size_t counter_bytes(const span_paged_desc_t* d) { return ((size_t)d->batch * d->kv_heads * sizeof(int32_t) + 255) & ~(size_t)255; }
 
 template <class Elt, int D, bool kSpans>
 int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, hipStream_t stream) {

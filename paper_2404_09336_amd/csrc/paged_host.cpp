@@ -109,7 +109,7 @@ PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, b
     at += (bytes + 255) & ~(size_t)255;
     return here;
   };
-  if (w.sliced || weights) part((size_t)d->batch * d->kv_heads * sizeof(int32_t));  // ticket counters, in every call's place for them
+  if (w.sliced || weights) part(counter_bytes(d));
   w.ml = part(w.sliced ? states * 2 * sizeof(float) : 0);
   w.acc = part(w.sliced ? states * (size_t)d->head_dim * sizeof(float) : 0);
   w.final_ml = part(weights ? (size_t)d->batch * d->heads * 2 * sizeof(float) : 0);
@@ -146,10 +146,12 @@ size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p) {
   return p.acc + (size_t)p.tiles * d->kv_heads * p.splits * kPromptTileRows * d->head_dim * sizeof(float);
 }
 
-// Of every (sequence, KV head) the number of rows that move and the pairs of their slots (8 bytes each).
+int32_t most_moves(const span_paged_desc_t* d) { return std::min(d->budget, std::max(capacity(d) - d->budget, 0)); }
+
+// The counters, and for long caches of every (sequence, KV head) the number of rows that move and the pairs of their slots (8 bytes each).
 size_t evict_workspace(const span_paged_desc_t* d) {
-  const size_t most = (size_t)std::min(d->budget, std::max(capacity(d) - d->budget, 0));
-  return (((size_t)d->batch * d->kv_heads * (2 + 2 * most) * sizeof(int32_t)) + 255) & ~(size_t)255;
+  const size_t lists = capacity(d) > kMostKeysHeld ? (size_t)d->batch * d->kv_heads * (2 + 2 * (size_t)most_moves(d)) * sizeof(int32_t) : 0;
+  return (counter_bytes(d) + lists + 255) & ~(size_t)255;
 }
 
 }  // namespace spanattn

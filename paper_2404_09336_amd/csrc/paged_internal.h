@@ -19,6 +19,9 @@ inline int32_t paged_whole(const span_paged_desc_t* d) { return d->dtype == SPAN
 
 int check_paged(const span_paged_desc_t* d);
 
+// Counters at the head of every workspace that has some, zero between calls: of every (sequence, KV head), then of every sequence.
+inline size_t counter_bytes(const span_paged_desc_t* d) { return ((size_t)d->batch * (d->kv_heads + 1) * sizeof(int32_t) + 255) & ~(size_t)255; }
+
 inline int page_shift(const span_paged_desc_t* d) { return __builtin_ctz((unsigned)d->page_size); }
 inline int32_t capacity(const span_paged_desc_t* d) { return d->table_pages * d->page_size; }  // positions of a sequence's table
 
@@ -50,6 +53,9 @@ struct PromptPlan {
 PromptPlan plan_prompt(const span_paged_desc_t* d);
 size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p);
 
+// An eviction of longer caches keeps lists in the workspace and moves their rows in a second launch.
+constexpr int32_t kMostKeysHeld = 32768;
+int32_t most_moves(const span_paged_desc_t* d);  // rows of a (sequence, KV head) that an eviction moves at most
 size_t evict_workspace(const span_paged_desc_t* d);
 
 }  // namespace spanattn

@@ -253,7 +253,7 @@ def prepare_paged_evict(k_pages, v_pages, block_table, ctx_lens, weights, budget
     _on_gpu(new_lens, "new_lens", torch.int32, (B,), device)
     desc = make_paged_desc(B, KV, KV, D, _dtype_code(k_pages), P, N, TP, sinks=sinks, budget=budget, recent=recent, stream=_stream(stream, device))
     _check(desc, "paged_evict")
-    workspace = _take_workspace(desc, PAGED_EVICT, workspace, device, False)
+    workspace = _take_workspace(desc, PAGED_EVICT, workspace, device, True)
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     args = (ctypes.byref(desc), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), ctx_lens.data_ptr(), weights.data_ptr(), ptr(positions),
             weights_out.data_ptr(), ptr(positions_out), new_lens.data_ptr())

@@ -153,6 +153,45 @@ def test_evict_long(n, cap_pages, gpu_device):
         pages = Pages([n, 2000], 1, 1, 64, 16, "f16", gpu_device, seed=3, table_pages=cap_pages)
 
 
+@pytest.mark.parametrize("batch,kv_heads", [(1, 1), (3, 5), (20, 16)])
+@pytest.mark.parametrize("cap_pages", [100, 400, 700, 1100])
+def test_evict_again_and_again_in_place(batch, kv_heads, cap_pages, gpu_device):
+    """One call after the other on one workspace, on the arrays themselves, with fewer and more (sequence, KV head) pairs than a card has CUs; the last
+    pages of the tables are free.  A sequence below the budget, one of one row, one without any."""
+    lens = ([1500, 900, 1, 0, 1201] * 4)[:batch]
+    pages = Pages(lens, kv_heads, kv_heads, 64, 16, "f16", gpu_device, seed=batch, table_pages=94)
+    table = torch.cat((pages.table, torch.full((batch, cap_pages - 94), -1, dtype=torch.int32)), dim=1).to(gpu_device)
+    cap, budget = cap_pages * 16, 1000
+    g = torch.Generator().manual_seed(cap)
+    weights = torch.rand((batch, kv_heads, cap), generator=g)
+    positions = torch.rand((batch, kv_heads, cap), generator=g).argsort(dim=-1).to(torch.int32)
+    K, V, ctx = pages.to("K", "V", "ctx")
+    w, pos = weights.to(gpu_device), positions.to(gpu_device)
+    call = span.prepare_paged_evict(K, V, table, ctx, w, budget, sinks=2, recent=30, positions=pos, weights_out=w, positions_out=pos, new_lens=ctx)
+    want = None
+    for _ in range(4):
+        for x, y in ((K, pages.K), (V, pages.V), (ctx, pages.ctx), (w, weights), (pos, positions)):
+            x.copy_(y)
+        call()
+        torch.cuda.synchronize()
+        got = [x.cpu() for x in (K, V, ctx, w, pos)]
+        assert got[2].tolist() == [min(n, budget) for n in lens]
+        if want is None:
+            want = got
+            for b in range(0, batch, 4):
+                for h in (0, kv_heads - 1):
+                    n = lens[b]
+                    to, of = evict(n, weights[b, h, :n].numpy(), positions[b, h, :n].numpy(), budget, 2, 30)
+                    expect = weights[b, h].clone()
+                    expect[to] = weights[b, h][of]
+                    expect[min(n, budget):n] = 0.0
+                    assert same(got[3][b, h], expect)
+                    for d, s in zip(to, of):
+                        assert same(got[0][pages.table[b, d // 16], h, d % 16], pages.K[pages.table[b, s // 16], h, s % 16])
+        for x, y in zip(got, want):
+            assert same(x, y)
+
+
 def test_a_life_of_a_cache(gpu_device):
     """Together, as a program uses them, step by step in one captured graph per step: rows go in, a token attends and the weights add up; an eviction
     whenever a cache outgrows its budget.  The plain form follows on the host."""
