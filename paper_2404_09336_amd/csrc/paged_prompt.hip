@@ -65,10 +65,11 @@ __device__ __forceinline__ TileName locate_tile(const PromptArgs& a, int y, int 
   TileName t = {-1, 0, 0, 0, 0};
   int before = 0;
   for (int c = 0; c < a.batch; c += 64) {
-    int begin = 0, count = 0;
+    int begin = 0, count = 0, len = 0;
     if (c + lane < a.batch) {
       begin = clampi(a.q_offsets[c + lane], 0, a.num_tokens);
       count = clampi(a.q_offsets[c + lane + 1], begin, a.num_tokens) - begin;
+      len = clampi(a.ctx_lens[c + lane], 0, a.max_len);
     }
     const int tiles = (int)((uint32_t)(count + a.tokens - 1) / (uint32_t)a.tokens);
     const int incl = before + wave_inclusive_scan(tiles);
@@ -79,7 +80,7 @@ __device__ __forceinline__ TileName locate_tile(const PromptArgs& a, int y, int 
       const int back = y - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(tiles, at));  // tile, from the last
       const int index = __builtin_amdgcn_readlane(tiles, at) - 1 - back;
       t.b = c + at;
-      t.len = clampi(__builtin_amdgcn_readfirstlane(a.ctx_lens[t.b]), 0, a.max_len);
+      t.len = __builtin_amdgcn_readlane(len, at);
       t.first = __builtin_amdgcn_readlane(begin, at) + index * a.tokens;
       t.tokens = min(a.tokens, all - index * a.tokens);
       t.pos = t.len - all + index * a.tokens;
@@ -162,16 +163,6 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     const uint32_t tk = (uint32_t)row / (uint32_t)group;
     return ((size_t)t.first + tk) * (size_t)(a.kv_heads * group) + (size_t)(h * group) + (size_t)((uint32_t)row - tk * (uint32_t)group);
   };
-  u32x4 qr[NP];
-  {
-    const char* src = (const char*)a.q + query_row(min(my_row, rows - 1)) * (size_t)ROWB + 16 * half;
-#pragma unroll
-    for (int mm = 0; mm < NP; ++mm) {
-      qr[mm] = *reinterpret_cast<const u32x4*>(src + 32 * mm);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) qr[mm][k] = Elt::scale_query(qr[mm][k], a.scale_log2e);
-    }
-  }
   const float post = Elt::post_scale(a.scale_log2e);
   constexpr float kShift = std::is_same<Elt, F16>::value ? 15.f : 0.f;  // weights times 2^15: fp16 then holds them down to 2^-39 of the heaviest
 
@@ -196,15 +187,15 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   u32x4 kx[NL], vx[NL];
   uint32_t outside;
   int pages = -1;  // lane l: the page of the wave's rows of tile 64 k + l, k the last that was looked up
+  const int origin = min(first_tile, max(all_tiles - 1, 0));  // the first tile, or some tile of a share without any
   auto look_up = [&](int i) {
-    const int entry = (tile_pos(min(i + lane, last_tile - 1)) + wave * RW) >> a.page_shift;
+    const int entry = (tile_pos(max(min(i + lane, last_tile - 1), 0)) + wave * RW) >> a.page_shift;
     pages = entry < a.table_pages ? table[entry] : -1;
   };
-  auto fetch = [&](int i) {
+  auto fetch_rows = [&](int i) {
     const int p = tile_pos(i) + wave * RW;  // the wave's rows of the tile lie in one page
     const int entry = p >> a.page_shift, in_page = p & ((1 << a.page_shift) - 1);
-    if ((i - first_tile) % 64 == 0) look_up(i);
-    const int page = __builtin_amdgcn_readlane(pages, (i - first_tile) % 64);
+    const int page = __builtin_amdgcn_readlane(pages, (i - origin) % 64);
     const bool good = (uint32_t)page < (uint32_t)a.num_pages;
     outside = !good && p < high ? 1u : 0u;
     const int there = good ? clampi(t.len - (entry << a.page_shift), 0, 1 << a.page_shift) : 0;  // rows of the page that are the sequence's
@@ -231,6 +222,24 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
       for (int i = 0; i < NL; ++i) vx[i] = __builtin_amdgcn_raw_buffer_load_b128(vp, base + 16u * (uint32_t)lane + 1024u * i, 0, 0);
     }
   };
+  auto fetch = [&](int i) {
+    if ((i - origin) % 64 == 0) look_up(i);
+    fetch_rows(i);
+  };
+  // Pages and queries are on their way together, then the first rows; only then are the queries waited for.
+  look_up(origin);
+  u32x4 qr[NP];
+  {
+    const char* src = (const char*)a.q + query_row(min(my_row, rows - 1)) * (size_t)ROWB + 16 * half;
+#pragma unroll
+    for (int mm = 0; mm < NP; ++mm) qr[mm] = *reinterpret_cast<const u32x4*>(src + 32 * mm);
+  }
+  fetch_rows(origin);
+#pragma unroll
+  for (int mm = 0; mm < NP; ++mm) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) qr[mm][k] = Elt::scale_query(qr[mm][k], a.scale_log2e);
+  }
   auto lay_down = [&](int buf, auto checked) {
     constexpr bool kChecked = decltype(checked)::value;
     if (lane == 0) reinterpret_cast<unsigned char*>(&s_out[buf])[wave] = (unsigned char)outside;
@@ -325,12 +334,16 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     if (!whole) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
+        // bit i: position pn + i counts, which `sees` says
+        const int pn = p0 + 32 * n;
+        auto first = [](int k) { return k >= 32 ? ~0u : (1u << max(k, 0)) - 1u; };
+        uint32_t bits = first(at - pn + 1);
+        if (a.window > 0) bits &= ~first(at - a.window + 1 - pn) | first(a.sinks - pn);
+        if constexpr (RW == 16) bits &= ~((out_bits >> (16 * n) & 1u) * 0xffffu | (out_bits >> (16 * n + 8) & 1u) * 0xffff0000u);
+        else bits &= ~(out_bits * 0xffu);
+        bits >>= 4 * half;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int i = 32 * n + 8 * (r / 4) + r % 4;  // (+ 4 half)
-          const bool ok = sees(p0 + i + 4 * half) && (out_bits >> (8 * (i / RW)) & 1u) == 0;
-          S[n][r] = ok ? S[n][r] : -INFINITY;
-        }
+        for (int r = 0; r < 16; ++r) S[n][r] = (bits >> (8 * (r / 4) + r % 4) & 1u) != 0 ? S[n][r] : -INFINITY;
       }
     }
     float mx = -INFINITY;
@@ -462,10 +475,10 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     }
     if (first_tile >= last_tile) return;
     if (kChecked) {
+      fetch(first_tile);
       if (tid < 4) s_wild[tid >> 1][tid & 1] = 0u;
       __syncthreads();
     }
-    fetch(first_tile);
     lay_down(0, checked);
     __syncthreads();
     int buf = 0;
