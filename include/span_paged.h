@@ -10,7 +10,7 @@
  * nothing throws or aborts across this ABI.  The device that owns desc->stream has to be the current one.  Every call
  * can be recorded into a HIP graph; lengths and block tables are read on the device by every replay.
  *
- * Layouts, all contiguous:
+ * Layouts, all contiguous and aligned to 16 bytes:
  *   k_pages, v_pages   desc->dtype  [num_pages, kv_heads, page_size, head_dim]
  *   block_table        int32        [batch, table_pages]: position p of sequence b is row p % page_size of page
  *                                   block_table[b, p / page_size].  A page outside [0, num_pages) is never read or

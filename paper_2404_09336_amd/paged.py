@@ -98,7 +98,16 @@ def _stream(stream, device):
     return torch.cuda.current_stream(device).cuda_stream if stream is None else stream
 
 
-def _take_workspace(desc, use, workspace, device, counters):
+def _allocations(stream, device):
+    """Context in which new tensors are allocated, filled and later handed on in the order of the call's stream, whichever the current one is."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device))
+
+
+def _take_workspace(desc, use, workspace, stream, device, counters):
     """Workspace of the call; one that the caller hands in must have been initialised (paged_workspace_init) where it has counters."""
     import torch
     need = paged_workspace_bytes(desc, use)
@@ -106,7 +115,8 @@ def _take_workspace(desc, use, workspace, device, counters):
         return None
     fresh = workspace is None
     if fresh:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        with _allocations(stream, device):
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
     elif workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {device}")
     desc.workspace = workspace.data_ptr()
@@ -158,7 +168,8 @@ def _prepare_decode(name, q, k_pages, v_pages, block_table, ctx_lens, spans, sca
     H = q.shape[1]
     _on_gpu(q, "q", k_pages.dtype, (B, H, D), device)
     if out is None:
-        out = torch.empty((B, H, D), dtype=torch.float32, device=device)
+        with _allocations(stream, device):
+            out = torch.empty((B, H, D), dtype=torch.float32, device=device)
     _on_gpu(out, "out", torch.float32, (B, H, D), device)
     weights_ptr = None if weights is None else _on_gpu(weights, "weights", torch.float32, (B, KV, TP * P), device)
     n_int = 0
@@ -172,7 +183,7 @@ def _prepare_decode(name, q, k_pages, v_pages, block_table, ctx_lens, spans, sca
                            tokens_per_seq=tokens_per_seq, stream=_stream(stream, device))
     _check(desc, name)
     use = (PAGED_DECODE if spans is None else PAGED_SPAN_DECODE) + (weights is not None)
-    workspace = _take_workspace(desc, use, workspace, device, True)
+    workspace = _take_workspace(desc, use, workspace, stream, device, True)
     lists = (ctx_lens,) if spans is None else spans
     args = (ctypes.byref(desc), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), *(t.data_ptr() for t in lists),
             float(scale), weights_ptr, out.data_ptr())
@@ -217,11 +228,12 @@ def prepare_paged_prompt_attn(q, k_pages, v_pages, block_table, ctx_lens, q_offs
     _on_gpu(q, "q", k_pages.dtype, (T, H, D), device)
     _on_gpu(q_offsets, "q_offsets", torch.int32, (B + 1,), device)
     if out is None:
-        out = torch.empty_like(q)
+        with _allocations(stream, device):
+            out = torch.empty_like(q)
     _on_gpu(out, "out", q.dtype, (T, H, D), device)
     desc = make_paged_desc(B, H, KV, D, _dtype_code(k_pages), P, N, TP, num_tokens=T, window=window, sinks=sinks, stream=_stream(stream, device))
     _check(desc, "paged_prompt_attn")
-    workspace = _take_workspace(desc, PAGED_PROMPT, workspace, device, False)
+    workspace = _take_workspace(desc, PAGED_PROMPT, workspace, stream, device, False)
     args = (ctypes.byref(desc), q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), ctx_lens.data_ptr(), q_offsets.data_ptr(),
             float(scale), out.data_ptr())
     keep = (q, k_pages, v_pages, block_table, ctx_lens, q_offsets, workspace)
@@ -241,19 +253,21 @@ def prepare_paged_evict(k_pages, v_pages, block_table, ctx_lens, weights, budget
     lib = _library()
     B, KV, P, D, N, TP, device = _cache(k_pages, v_pages, block_table, ctx_lens)
     _on_gpu(weights, "weights", torch.float32, (B, KV, TP * P), device)
-    weights_out = torch.zeros_like(weights) if weights_out is None else weights_out
+    with _allocations(stream, device):
+        weights_out = torch.zeros_like(weights) if weights_out is None else weights_out
+        new_lens = torch.empty_like(ctx_lens) if new_lens is None else new_lens
+        if positions is not None and positions_out is None:
+            positions_out = torch.full_like(positions, -1)
     _on_gpu(weights_out, "weights_out", torch.float32, (B, KV, TP * P), device)
     if positions is not None:
         _on_gpu(positions, "positions", torch.int32, (B, KV, TP * P), device)
-        positions_out = torch.full_like(positions, -1) if positions_out is None else positions_out
         _on_gpu(positions_out, "positions_out", torch.int32, (B, KV, TP * P), device)
     elif positions_out is not None:
         raise ValueError("positions_out needs positions")
-    new_lens = torch.empty_like(ctx_lens) if new_lens is None else new_lens
     _on_gpu(new_lens, "new_lens", torch.int32, (B,), device)
     desc = make_paged_desc(B, KV, KV, D, _dtype_code(k_pages), P, N, TP, sinks=sinks, budget=budget, recent=recent, stream=_stream(stream, device))
     _check(desc, "paged_evict")
-    workspace = _take_workspace(desc, PAGED_EVICT, workspace, device, True)
+    workspace = _take_workspace(desc, PAGED_EVICT, workspace, stream, device, True)
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     args = (ctypes.byref(desc), k_pages.data_ptr(), v_pages.data_ptr(), block_table.data_ptr(), ctx_lens.data_ptr(), weights.data_ptr(), ptr(positions),
             weights_out.data_ptr(), ptr(positions_out), new_lens.data_ptr())
