@@ -401,6 +401,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
       }
     }
   };
+  const __amdgpu_buffer_rsrc_t pair_scores = slab_resource(a.scores + bh * (size_t)group * (size_t)a.max_len, kWeights ? (uint32_t)group * (uint32_t)a.max_len * 4u : 0u);
   // Scores -> weights; moves the state's maximum and adds to its sum.  v0: virtual position of the step's first row.
   auto softmax_step = [&](f32x4 (&sc)[S], int v0, const TileRows& tr) {
     if (!tr.plain) {
@@ -410,13 +411,13 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         for (int t = 0; t < 4; ++t) sc[s][t] = (tr.ok[s] >> (4 * c4 + t)) & 1u ? sc[s][t] : -INFINITY;
       }
     }
-    if (kWeights && qi < group) {
-      float* at = a.scores + (bh * (size_t)group + (size_t)qi) * (size_t)a.max_len + (size_t)(v0 + 4 * c4);
+    if constexpr (kWeights) {
+      // (Stores without a branch: the waits for the rows behind them are counted.  What is nobody's, or the next slice's, goes out of the descriptor's range.)
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        // (a quad that begins past the last position belongs to nobody, or to the next slice)
-        const int v = kWavesPerBlock * kUnit * s;  // the wave's next unit
-        if (v0 + v + 4 * c4 < slice_begin + cnt) *reinterpret_cast<f32x4*>(at + v) = sc[s];
+        const int v = v0 + kWavesPerBlock * kUnit * s + 4 * c4;  // (s > 0: the wave's next unit)
+        const uint32_t at = qi < group && v < slice_begin + cnt ? ((uint32_t)qi * (uint32_t)a.max_len + (uint32_t)v) * 4u : ~15u;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, sc[s]), pair_scores, at, 0, 0);
       }
     }
     float mx = -INFINITY;
