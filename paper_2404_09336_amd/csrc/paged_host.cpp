@@ -120,9 +120,18 @@ PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, b
   return w;
 }
 
-// Workgroups from which on a prompt call's tiles are not shared out, and that it aims at where they are.
-constexpr int64_t kPromptFewTiles = 256, kPromptWorkgroups = 512;
-constexpr int64_t kPromptLeastPositions = 256;  // of a share
+// A prompt call of fewer workgroups than CUs has its tiles' positions shared out, among as many workgroups as kPromptWorkgroups allows and so that each has
+// about kPromptLeastPositions of a full table at least; a second launch joins the shares.  fp32 products take eight times as long, so that a share of two steps pays and one workgroup
+// keeps a CU busy.  us, bf16 / fp32:
+//   never shared                 200 new of 4000, 32 heads on 8 of 128   99 /  -     64 of 3000, 8 heads of 128, fp32     - / 416
+//   256 workgroups                                                       39 /  -                                          - /  29 (64 positions at least)
+//   512 workgroups                                                       36 /  -                                          - /  35
+//   1024 workgroups                                                      48 /  -
+//   128, 192, 256 at least (512) 100 of 1000, 8 heads of 128      13, 14, 16 /  -     10 of 6000, 5 heads of 64    15, 14, 14 /  -
+//   64, 256 at least (fp32)      100 of 1000, 8 heads of 128           - / 22, 46
+constexpr int64_t kPromptFewTiles = 256;
+constexpr int64_t kPromptWorkgroups16 = 512, kPromptLeastPositions16 = 192;
+constexpr int64_t kPromptWorkgroups32 = 256, kPromptLeastPositions32 = 64;
 
 PromptPlan plan_prompt(const span_paged_desc_t* d) {
   PromptPlan p;
@@ -134,7 +143,11 @@ PromptPlan plan_prompt(const span_paged_desc_t* d) {
   int64_t most = capacity(d);
   if (d->window > 0) most = std::min<int64_t>(most, (int64_t)d->window + d->sinks + p.tokens);
   int64_t splits = 1;
-  if (workgroups > 0 && workgroups < kPromptFewTiles) splits = std::min(kPromptWorkgroups / workgroups, ceil_div(most, kPromptLeastPositions));
+  const bool fp32 = d->dtype == SPAN_F32;
+  if (workgroups > 0 && workgroups < kPromptFewTiles) {
+    const int64_t least = fp32 ? kPromptLeastPositions32 : kPromptLeastPositions16;
+    splits = std::min((fp32 ? kPromptWorkgroups32 : kPromptWorkgroups16) / workgroups, (most + least / 2) / least);
+  }
   p.splits = (int32_t)std::max<int64_t>(splits, 1);
   const size_t rows = p.splits > 1 ? (size_t)workgroups * p.splits * kPromptTileRows : 0;
   p.acc = (rows * 2 * sizeof(float) + 255) & ~(size_t)255;

@@ -10,6 +10,12 @@
 //     the positions of 16 in that order, and is read like K.
 // The next tile's rows are on their way to registers while this one is computed, and go to the other half of LDS after it: one barrier per tile.
 // A row of K or V past the sequence's length is not read (the buffer descriptor of a page ends there) and counts as zeros.
+//
+// What bounds it: the matrix cores and, between their runs, the vector instructions of the softmax - a wave's own do not run beside its products, only the other
+// wave's of its SIMD do.  One prompt of 8192 tokens, 32 query heads on 8 KV heads of 128, bf16: 596 us, 920 TFLOP/s of the 1208 that a product of 8192^3 reaches
+// here; six chunks with a window of 1024, fp16: 188 us, 637 TFLOP/s (18 tiles a workgroup, of which 4 are cut by the window, the sinks or the diagonal).
+// Tried and slower (us of those two, against 602 / 201 then): 16 query rows a wave and twice the waves 677 / 222 (twice the reads of LDS); a half tile's softmax among
+// the other half's products in one wave 661 / 223; 256 rows a workgroup whose two halves take turns 575 / 231 (faster long, slower where tiles are cut).
 #include "paged_device.h"
 
 namespace spanattn {
@@ -565,18 +571,34 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptArgs a) {
   const size_t slot0 = ((size_t)blockIdx.y * a.kv_heads + h) * (size_t)a.splits;
   float M = -INFINITY, L = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const size_t at = (slot0 + (size_t)s) * kPromptRows + (size_t)row;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * at);
-    const f32x4 os = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + column);
-    if (ml[1] == 0.f) continue;  // (nothing seen there; a NaN sum counts)
-    const float before = M;
-    M = fmaxf(M, ml[0]);
-    const float safe = M == -INFINITY ? 0.f : M;
-    const float old = __builtin_amdgcn_exp2f((before - safe) * post), w = __builtin_amdgcn_exp2f((ml[0] - safe) * post);
-    L = fmaf(L, old, w * ml[1]);
+  constexpr int kAhead = 8;  // states on their way at once
+  for (int s0 = 0; s0 < a.splits; s0 += kAhead) {
+    f32x2 ml[kAhead];
+    f32x4 os[kAhead];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) o[k] = fmaf(o[k], old, w * os[k]);
+    for (int k = 0; k < kAhead; ++k) {
+      const size_t at = (slot0 + (size_t)min(s0 + k, a.splits - 1)) * kPromptRows + (size_t)row;  // (past the end: the last once more, unused)
+      ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + 2 * at);
+      os[k] = *reinterpret_cast<const f32x4*>(a.part_acc + at * D + column);
+    }
+    const float before = M;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (s0 + k >= a.splits) ml[k][1] = 0.f;
+      if (ml[k][1] != 0.f) M = fmaxf(M, ml[k][0]);  // (0: nothing seen there; a NaN sum counts)
+    }
+    const float safe = M == -INFINITY ? 0.f : M, old = __builtin_amdgcn_exp2f((before - safe) * post);
+    L *= old;
+    o *= old;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (ml[k][1] != 0.f) {
+        const float w = __builtin_amdgcn_exp2f((ml[k][0] - safe) * post);
+        L = fmaf(w, ml[k][1], L);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = fmaf(w, os[k][c], o[c]);
+      }
+    }
   }
   const float sum = L != 0.f ? L : 1.f;
   const uint32_t tk = (uint32_t)row / (uint32_t)a.group;
