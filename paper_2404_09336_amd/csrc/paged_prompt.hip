@@ -229,7 +229,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     }
   };
   auto fetch = [&](int i) {
-    if ((i - origin) % 64 == 0) look_up(i);
+    if (i > origin && (i - origin) % 64 == 0) look_up(i);
     fetch_rows(i);
   };
   // Pages and queries are on their way together, then the first rows; only then are the queries waited for.
@@ -481,7 +481,8 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     }
     if (first_tile >= last_tile) return;
     if (kChecked) {
-      fetch(first_tile);
+      look_up(origin);
+      fetch_rows(origin);
       if (tid < 4) s_wild[tid >> 1][tid & 1] = 0u;
       __syncthreads();
     }
@@ -491,6 +492,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     for (int i = first_tile; i < last_tile; ++i) {
       fetch(min(i + 1, last_tile - 1));  // (the last tile a second time rather than a branch, which would cost copies of all these registers)
       compute(buf, tile_pos(i), checked);
+      if (i + 1 == last_tile) break;
       if (kChecked) {
         __syncthreads();
         if (tid < 2) s_wild[buf][tid] = 0u;  // (for the tile after next)
@@ -499,6 +501,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
       __syncthreads();
       buf ^= 1;
     }
+    if (kChecked) __syncthreads();  // (as the vote does behind the other pass: nobody reads LDS any more)
   };
   walk(std::false_type{});
   {
