@@ -308,6 +308,10 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   bool large = false;
   float ref = -INFINITY, lsum = 0.f;  // reference of the weights: the largest unscaled score; this lane's share of their sum
   f32x16 O[kBlocks];
+  // A weight is exp2(score * post + shift), shift = kShift - reference * post rounded.  What the rounding leaves is a factor exp2(slack) of all weights of one
+  // reference: it goes out with their sum, but where the reference moves or shares are joined it has to be taken into account (without that, fp32 scores near 2^13 that
+  // lie close to one another gave outputs off by 3e-5, near 2^21 by 7e-3).
+  float slack = 0.f;
   auto sees = [&](int p) { return p <= at && (a.window == 0 || p > at - a.window || p < a.sinks); };
 
   const int v_lane = col * kVRow + 16 * (half ^ (col >> 4));
@@ -361,16 +365,17 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     if (__builtin_amdgcn_ballot_w64(mx > ref) != 0) {
       const Swapped sw = swap_lanes<32>(mx, mx);
       const float ref_new = fmaxf(ref, fmaxf(sw.first, sw.second)), safe = ref_new == -INFINITY ? 0.f : ref_new;
-      const float alpha = __builtin_amdgcn_exp2f((ref - safe) * post);
+      shift = kShift - safe * post;
+      large = __builtin_amdgcn_ballot_w64(!(fabsf(shift) < kLargeShift)) != 0;
+      const float slack_new = large ? 0.f : fmaf(safe, post, shift) - kShift;
+      const float alpha = __builtin_amdgcn_exp2f(fmaf(ref - safe, post, slack_new - slack));
       ref = ref_new;
+      slack = slack_new;
       lsum *= alpha;
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e) O[e] *= alpha;
-      shift = kShift - safe * post;
-      large = __builtin_amdgcn_ballot_w64(!(fabsf(shift) < kLargeShift)) != 0;
     }
-    // A weight is exp2(score * post + shift), shift = -reference * post rounded: its rounding is a factor of all weights and goes out with their sum.
-    // Where it is no longer small the difference from the reference is taken first, which is exact.
+    // Where the shift's rounding is no longer small the difference from the reference is taken first, which is exact.
     if (__builtin_expect(large, 0)) {
       const float safe = ref == -INFINITY ? 0.f : ref;
 #pragma unroll
@@ -473,6 +478,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     ref = -INFINITY;
     lsum = 0.f;
     shift = kShift;
+    slack = 0.f;
     large = false;
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e) {
@@ -518,6 +524,10 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   lsum = both.first + both.second;
   if (a.splits > 1) {
     if (my_row < rows) {
+      const float level = __builtin_amdgcn_exp2f(-slack);  // (the merge takes a share's weights relative to its reference)
+      lsum *= level;
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) O[e] *= level;
       const size_t slot = ((size_t)blockIdx.y * a.kv_heads + h) * (size_t)a.splits + (size_t)split;
       const size_t row = slot * kPromptRows + (size_t)my_row;
       if (half == 0) *reinterpret_cast<f32x2*>(a.part_ml + 2 * row) = f32x2{ref, lsum};
