@@ -15,7 +15,9 @@
  *   block_table        int32        [batch, table_pages]: position p of sequence b is row p % page_size of page
  *                                   block_table[b, p / page_size].  A page outside [0, num_pages) is never read or
  *                                   written: its positions are attended by nobody, rows for it are dropped.
- *   ctx_lens           int32 [batch]: positions in use; clamped to [0, table_pages * page_size]
+ *   ctx_lens           int32 [batch]: positions in use.  Those from table_pages * page_size on have no row: a token there keeps
+ *                                   its position (what a window hides from it goes by that), and nobody attends it.  A negative
+ *                                   length counts as 0
  *   q_offsets          int32 [batch + 1]: rows q_offsets[b] .. q_offsets[b + 1] - 1 of q / k_new / v_new / out are the
  *                                   new tokens of sequence b, the last of them at position ctx_lens[b] - 1 (ctx_lens
  *                                   counts them already); not decreasing, within [0, num_tokens].  Rows that belong to
@@ -88,8 +90,8 @@ int paged_workspace_init(const span_paged_desc_t* desc);
  *   q_offsets    : NULL = one token per sequence (num_tokens == batch)
  *   seen         : device int32 [batch] or NULL: tokens of the sequence so far, the new ones among them; NULL = ctx_lens
  *                  (differs from it once rows were evicted)
- * Rows whose position lies outside [0, table_pages * page_size) are dropped, and those of a page outside the pool.  Pages written
- * to must belong to one sequence only.
+ * Rows whose position lies outside [0, table_pages * page_size) are dropped, so that a full table keeps what it holds, and so are
+ * those of a page outside the pool.  Pages written to must belong to one sequence only.
  */
 int paged_append(const span_paged_desc_t* desc, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
                  const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, int32_t* positions,
@@ -97,7 +99,8 @@ int paged_append(const span_paged_desc_t* desc, const void* k_new, const void* v
 
 /*
  * Attention of one new token per sequence (its row already appended) over S_b, the positions
- *   max(0, n - window) <= p < n  (all p < n for window 0)  and  p < min(sinks, n),      n = ctx_lens[b]:
+ *   max(0, n - window) <= p < n  (all p < n for window 0)  and  p < min(sinks, n),      n = ctx_lens[b],
+ * that the table has a row for:
  *   s_j = scale * q[b, i, :] . K[b, i / group, j, :]       out[b, i, :] = sum_j softmax_j(s)_j V[b, i / group, j, :]
  *   q   : device, desc->dtype, [batch, heads, head_dim]      out : device fp32 [batch, heads, head_dim]
  *   weights : device or NULL; if given, weights[b, h, j] += sum over the query heads of KV head h of softmax_j, j in S_b
@@ -139,7 +142,7 @@ int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, const void* 
  *   positions       : device or NULL: slot i holds position i
  *   weights_out, positions_out (the latter NULL if positions is): what the slots below ctx_lens[b] hold afterwards, weight 0
  *                     and position -1 in those that fell free; may be the arrays themselves
- *   new_lens        : device int32 [batch]: min(ctx_lens[b], budget); may be ctx_lens itself
+ *   new_lens        : device int32 [batch]: min(ctx_lens[b], table_pages * page_size, budget); may be ctx_lens itself
  * Pages of a sequence must differ from one another and belong to it alone.
  */
 int paged_evict(const span_paged_desc_t* desc, void* k_pages, void* v_pages, const int32_t* block_table,

@@ -62,9 +62,9 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
     end = a.q_offsets[b + 1];
   }
   b = __builtin_amdgcn_readfirstlane(b);
-  const int len = clampi(a.ctx_lens[b], 0, a.max_len);
-  const int p = __builtin_amdgcn_readfirstlane(len - end + t);
-  if (p < 0) return;
+  const int len = a.ctx_lens[b];
+  const int p = __builtin_amdgcn_readfirstlane((int)((uint32_t)len - (uint32_t)end + (uint32_t)t));
+  if ((uint32_t)p >= (uint32_t)a.max_len) return;  // no place in the table: ahead of its first position, or the table is full
   if (a.positions != nullptr && c == 0) {
     const int position = (a.seen != nullptr ? a.seen[b] : len) - end + t;
     for (int h = lane; h < a.kv_heads; h += 64) a.positions[((size_t)b * a.kv_heads + h) * (size_t)a.max_len + p] = position;

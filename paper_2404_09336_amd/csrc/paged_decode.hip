@@ -70,8 +70,8 @@ struct Slice {
 __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lane) {
   int len = 0, n = 0;
   auto fetch = [&](int c) {
-    len = c + lane < a.batch ? clampi(a.ctx_lens[c + lane], 0, a.max_len) : 0;
-    n = seen_by_last(len, a.window, a.sinks).count;
+    len = c + lane < a.batch ? a.ctx_lens[c + lane] : 0;
+    n = seen_by_last(len, a.max_len, a.window, a.sinks).count;
   };
   uint32_t all = 0, longest = 1;
   for (int c = 0; c < a.batch; c += 64) {
@@ -244,8 +244,8 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     fetch_first(a, intervals, lane);
     n_total = min(count_positions(a, intervals, wave, lane, s_u.st.tab), a.max_len);
   } else {
-    if (a.room == 0) sl.len = clampi(__builtin_amdgcn_readfirstlane(a.ctx_lens[b]), 0, a.max_len);
-    seen = seen_by_last(sl.len, a.window, a.sinks);
+    if (a.room == 0) sl.len = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]);
+    seen = seen_by_last(sl.len, a.max_len, a.window, a.sinks);
     n_total = seen.count;
   }
   n_total = __builtin_amdgcn_readfirstlane(n_total);
@@ -683,7 +683,7 @@ __global__ __launch_bounds__(256) void weights_kernel(const PagedArgs a) {
   int n;
   if constexpr (kSpans) n = a.counts[b];
   else {
-    seen = seen_by_last(clampi(a.ctx_lens[b], 0, a.max_len), a.window, a.sinks);
+    seen = seen_by_last(a.ctx_lens[b], a.max_len, a.window, a.sinks);
     n = seen.count;
   }
   if (v0 < n) add_weights<Elt, kSpans>(a, seen, n, b, h, v0);

@@ -27,15 +27,16 @@ __device__ __forceinline__ int pool_row(const int32_t* table_of_b, int p, int pa
   return (uint32_t)page < (uint32_t)num_pages ? (page << page_shift) + (p & ((1 << page_shift) - 1)) : -1;
 }
 
-// Positions that the token at position n - 1 sees: [0, sinks) and [low, n).
+// Positions that the token at position n - 1 sees: [0, sinks) and from `low` on, of those below n that the table has.
 struct Seen {
   int sinks, low, count;
 };
-__device__ __forceinline__ Seen seen_by_last(int n, int window, int sinks) {
+__device__ __forceinline__ Seen seen_by_last(int n, int max_len, int window, int sinks) {
+  const int held = clampi(n, 0, max_len);
   Seen s;
-  s.low = window > 0 ? max(n - window, 0) : 0;
+  s.low = window > 0 ? clampi(max(n, 0) - window, 0, held) : 0;
   s.sinks = min(sinks, s.low);
-  s.count = n - s.low + s.sinks;
+  s.count = held - s.low + s.sinks;
   return s;
 }
 

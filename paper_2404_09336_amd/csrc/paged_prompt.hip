@@ -63,7 +63,7 @@ struct PromptShape {
 
 struct TileName {
   int b, first, tokens, pos;  // sequence; first row of q, tokens, position of the first
-  int len;
+  int len;                    // positions that the table has
 };
 
 // Tile y: sequences in order, each in tiles of `a.tokens` tokens from its last token back (the tiles with most positions start first).
@@ -75,7 +75,7 @@ __device__ __forceinline__ TileName locate_tile(const PromptArgs& a, int y, int 
     if (c + lane < a.batch) {
       begin = clampi(a.q_offsets[c + lane], 0, a.num_tokens);
       count = clampi(a.q_offsets[c + lane + 1], begin, a.num_tokens) - begin;
-      len = clampi(a.ctx_lens[c + lane], 0, a.max_len);
+      len = max(a.ctx_lens[c + lane], 0);
     }
     const int tiles = (int)((uint32_t)(count + a.tokens - 1) / (uint32_t)a.tokens);
     const int incl = before + wave_inclusive_scan(tiles);
@@ -86,10 +86,11 @@ __device__ __forceinline__ TileName locate_tile(const PromptArgs& a, int y, int 
       const int back = y - (__builtin_amdgcn_readlane(incl, at) - __builtin_amdgcn_readlane(tiles, at));  // tile, from the last
       const int index = __builtin_amdgcn_readlane(tiles, at) - 1 - back;
       t.b = c + at;
-      t.len = __builtin_amdgcn_readlane(len, at);
+      const int end = __builtin_amdgcn_readlane(len, at);  // tokens keep their positions where the table ends before them
+      t.len = min(end, a.max_len);
       t.first = __builtin_amdgcn_readlane(begin, at) + index * a.tokens;
       t.tokens = min(a.tokens, all - index * a.tokens);
-      t.pos = t.len - all + index * a.tokens;
+      t.pos = end - all + index * a.tokens;
       break;
     }
     before = __builtin_amdgcn_readlane(incl, 63);
@@ -164,7 +165,7 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   const int rows = t.tokens * group;
   const int my_row = 32 * wave + col;
   const int tok = min((int)((uint32_t)my_row / (uint32_t)group), t.tokens - 1);
-  const int at = t.pos + tok;
+  const int at = t.pos + tok, top = min(at, t.len - 1);  // its position, and the last that it may see
   auto query_row = [&](int row) {  // row (< rows) of the tile in q and out, in rows of D
     const uint32_t tk = (uint32_t)row / (uint32_t)group;
     return ((size_t)t.first + tk) * (size_t)(a.kv_heads * group) + (size_t)(h * group) + (size_t)((uint32_t)row - tk * (uint32_t)group);
@@ -173,8 +174,9 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   constexpr float kShift = std::is_same<Elt, F16>::value ? 15.f : 0.f;  // weights times 2^15: fp16 then holds them down to 2^-39 of the heaviest
 
   // Positions the tile's tokens see together: [0, sinks) and [low, high).  Cache tiles: the sinks' first, then the others.
-  const int high = t.pos + t.tokens;
-  const int low = a.window > 0 ? max(t.pos - a.window + 1, 0) : 0;
+  const int high = min(t.pos + t.tokens, t.len);
+  const int window = t.pos + t.tokens > a.window ? a.window : 0;  // 0: it hides nothing from any of them
+  const int low = window > 0 ? max(t.pos - window + 1, 0) : 0;
   const int sinks = min(a.sinks, low);
   const int sink_tiles = (sinks + KT - 1) / KT;
   const int from = max(low / KT, sink_tiles), to = max((max(high, 0) + KT - 1) / KT, from);
@@ -312,13 +314,13 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
   // reference: it goes out with their sum, but where the reference moves or shares are joined it has to be taken into account (without that, fp32 scores near 2^13 that
   // lie close to one another gave outputs off by 3e-5, near 2^21 by 7e-3).
   float slack = 0.f;
-  auto sees = [&](int p) { return p <= at && (a.window == 0 || p > at - a.window || p < a.sinks); };
+  auto sees = [&](int p) { return p <= top && (window == 0 || p > at - window || p < a.sinks); };
 
   const int v_lane = col * kVRow + 16 * (half ^ (col >> 4));
   auto compute = [&](int buf, int p0, auto checked) {
     constexpr bool kChecked = decltype(checked)::value;
     if (!wave_works || p0 > wave_last) return;
-    if (a.window > 0 && p0 + KT - 1 <= wave_first - a.window && p0 >= a.sinks) return;
+    if (window > 0 && p0 + KT - 1 <= wave_first - window && p0 >= a.sinks) return;
     constexpr f32x16 kZero = {};
     f32x16 S[NB];
 #pragma unroll
@@ -340,15 +342,15 @@ __attribute__((amdgpu_waves_per_eu(2, 2))) void prompt_kernel(const PromptArgs a
     }
     reads_ahead<NB * NP, kHalf ? 1 : 4, kAhead>();
     const uint32_t out_bits = (uint32_t)__builtin_amdgcn_readfirstlane((int)s_out[buf]);
-    const bool whole = p0 + KT - 1 <= wave_first && (a.window == 0 || p0 > wave_last - a.window || p0 + KT <= a.sinks) && out_bits == 0;
+    const bool whole = p0 + KT - 1 <= min(wave_first, t.len - 1) && (window == 0 || p0 > wave_last - window || p0 + KT <= a.sinks) && out_bits == 0;
     if (!whole) {
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         // bit i: position pn + i counts, which `sees` says
         const int pn = p0 + 32 * n;
         auto first = [](int k) { return k >= 32 ? ~0u : (1u << max(k, 0)) - 1u; };
-        uint32_t bits = first(at - pn + 1);
-        if (a.window > 0) bits &= ~first(at - a.window + 1 - pn) | first(a.sinks - pn);
+        uint32_t bits = first(top - pn + 1);
+        if (window > 0) bits &= ~first(at - window + 1 - pn) | first(a.sinks - pn);
         if constexpr (RW == 16) bits &= ~((out_bits >> (16 * n) & 1u) * 0xffffu | (out_bits >> (16 * n + 8) & 1u) * 0xffff0000u);
         else bits &= ~(out_bits * 0xffu);
         bits >>= 4 * half;
@@ -669,7 +671,7 @@ extern "C" int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, c
   a.tokens = p.tokens;
   a.tiles = p.tiles;
   a.splits = p.splits;
-  a.window = desc->window < a.max_len ? desc->window : 0;  // (a window of the whole table hides nothing)
+  a.window = desc->window;
   a.sinks = desc->sinks < a.max_len ? desc->sinks : a.max_len;
   a.scale_log2e = scale * 1.4426950408889634f;
   hipStream_t stream = (hipStream_t)desc->stream;
