@@ -242,7 +242,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     words.last = __builtin_amdgcn_readfirstlane(a.offsets[b + 1]);
     intervals = interval_range(a, words);
     fetch_first(a, intervals, lane);
-    n_total = min(count_positions(a, intervals, wave, lane, s_u.st.tab), a.max_len);
+    n_total = clampi(count_positions(a, intervals, wave, lane, s_u.st.tab), 0, a.max_len);
   } else {
     if (a.room == 0) sl.len = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]);
     seen = seen_by_last(sl.len, a.max_len, a.window, a.sinks);
@@ -277,7 +277,7 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
       if (r < wn) {
         const int v = vrow(w0 + r);
         int p;
-        if constexpr (kSpans) p = s_row[wave][r];
+        if constexpr (kSpans) p = clampi(s_row[wave][r], 0, a.max_len - 1);  // (a list whose positions add up past 32 bits leaves rows that the walk does not find)
         else p = v < seen.sinks ? v : v - seen.sinks + seen.low;
         x = pool_row(table, p, a.page_shift, a.num_pages);
         // (who adds up weights reads his own entries back; the heads' are equal)
