@@ -9,7 +9,7 @@
 //   * The slices are found on the device from the lengths themselves (locate_slice): a captured call stays level when lengths grow.
 //   * Weights per position (for an eviction) need the final maxima and sums: the scores go to the workspace as they are taken and a
 //     second kernel turns them into weights, 4 bytes a score against the 2 * head_dim * element bytes of a row.  Where no sequence is cut
-//     the workgroup does that itself.
+//     and the positions are few (kPagedOwnWeights) the workgroup does that itself.
 // What bounds it: memory, and for short calls the chain of trips before the first rows and of the hand-over behind the last.  64 sequences
 // of 512 .. 4096 positions, 32 query heads on 8 KV heads of 128, bf16: 104 us, 6.0 TB/s; a window of 1024 over 32 of them, fp16: 26.7 us,
 // 5.0 TB/s; 4 of 8000 .. 32768: 55.9 us, 5.6 TB/s, with weights 67 (the scores' 10 MB cost 8 us on their way out and 5.4 in the second
@@ -34,7 +34,7 @@ struct PagedArgs : LaunchArgs {  // heads: KV heads; max_len: positions of a seq
   int32_t* counts;           // span form with weights: [batch] attended positions
   int32_t* list;             // ... and [batch, max_len] the positions themselves
   float* weights;
-  int32_t weights_here;      // 1: the workgroup that attends adds up the weights too (every pair is one workgroup)
+  int32_t weights_here;      // 1: the workgroup that attends adds up the weights too (PagedPlan::own_weights)
 };
 struct PagedArgsPlain : PagedArgs {
   static constexpr bool kHasTable = false;
@@ -60,7 +60,7 @@ struct Slice {
   int b, split, nsl, y0, len;  // sequence, slice within it, slices of it, slot of its first slice; its length (locate_slice)
 };
 
-// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than kPagedWhole, T whole steps and
+// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than `whole`, T whole steps and
 // kPagedLeastSlice at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
 // many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice well above the
 // mean, which is what the whole call waits for then, `more_room` is tried.  Every workgroup works it out for itself: one load of the lengths,
@@ -754,7 +754,7 @@ int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const
   a.heads = d->kv_heads;
   a.max_len = a.max_tokens = capacity(d);
   a.num_intervals = d->num_intervals;
-  a.num_splits = p.splits;
+  a.num_splits = p.cut ? p.splits : 1;
   a.scale_log2e = scale * 1.4426950408889634f;
   a.block_table = block_table;
   a.table_pages = d->table_pages;
@@ -764,7 +764,7 @@ int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const
   a.batch = d->batch;
   a.window = d->window;
   a.sinks = d->sinks;
-  a.room = p.room;
+  a.room = p.cut ? p.room : 0;
   a.more_room = p.rows;
   a.whole = paged_whole(d);
   a.final_ml = weights ? (float*)(at + w.final_ml) : nullptr;
@@ -772,7 +772,7 @@ int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const
   a.list = weights && kSpans ? (int32_t*)(at + w.list) : nullptr;
   a.scores = weights ? (float*)(at + w.scores) : nullptr;
   a.weights = weights;
-  a.weights_here = weights && !w.sliced ? 1 : 0;
+  a.weights_here = weights && p.own_weights ? 1 : 0;
   hipStream_t stream = (hipStream_t)d->stream;
   const bool d128 = d->head_dim == 128;
   switch (d->dtype) {

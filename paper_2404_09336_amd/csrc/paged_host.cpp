@@ -28,8 +28,14 @@ static int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 // Workgroups a one-token call aims at: two per CU, and as many as run at once (four) where that leaves slices of very different length.
 constexpr int64_t kPagedWorkgroups = 512, kPagedMoreWorkgroups = 1024;
 
+// A dense call that is never cut leaves the weights to a second launch beyond so many positions of all (sequence, KV head) pairs: the launch costs some 3 us, a
+// workgroup's own pass over its positions a trip to memory for each 1024.  us, second launch -> own: 128 x 8 pairs in a window of 512 (0.5 M positions at most) 54.8 ->
+// 51.6; 64 x 32 of up to 512 (1.0 M) 61.9 -> 60.9; of up to 1472 (3.0 M) 100.5 -> 102.0; of up to 2048 134.8 -> 138.3; 40 x 32 of up to 2000 (2.6 M), four query
+// heads each, 115.5 -> 110.7.
+constexpr int64_t kPagedOwnWeights = 3 << 19;
+
 PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
-  PagedPlan p = {0, 1, false, 0};
+  PagedPlan p = {0, 1, false, 0, false, false};
   const int64_t cap = capacity(d), whole = paged_whole(d);
   const int64_t room = std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads), more_room = std::max<int64_t>(1, kPagedMoreWorkgroups / d->kv_heads);
   auto uniform = [&](int64_t splits) {
@@ -37,6 +43,8 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
     splits = std::min<int64_t>(splits, 65535 / d->batch);  // grid.y
     p.splits = (int32_t)std::max<int64_t>(splits, 1);
     p.rows = p.splits * d->batch;
+    p.cut = p.splits > 1;
+    p.own_weights = !p.cut;
     return p;
   };
   if (d->num_splits > 0) return uniform(d->num_splits);
@@ -47,6 +55,8 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
     p.room = (int32_t)room;
     p.splits = 2;
     p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(most, kPagedLeastSlice) * d->batch));
+    p.cut = more_room > d->batch;  // (otherwise one slice each whatever the lengths; the workspace is that of other batches of the shape)
+    p.own_weights = !p.cut && most * d->batch * d->kv_heads <= kPagedOwnWeights;
     return p;
   }
   if (d->tokens_per_seq && d->batch <= kMaxPlanSlices) {  // as locate_slice does
@@ -88,7 +98,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
           for (int64_t s = 0; s < nsl; ++s) table[at++] = pack_slice((uint32_t)b, (uint32_t)s, (uint32_t)nsl);
         }
       }
-      p.table = true;
+      p.table = p.cut = true;
       p.splits = (int32_t)most;
       p.rows = (int32_t)y;
       return p;

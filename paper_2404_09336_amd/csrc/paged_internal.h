@@ -31,6 +31,8 @@ struct PagedPlan {
   int32_t splits;    // room 0: slices of every sequence, or the most of any (table)
   bool table;        // slices from a table of pack_slice entries
   int32_t rows;      // grid.y: slices of all sequences (upper bound)
+  bool cut;          // some lengths give some sequence several slices
+  bool own_weights;  // the workgroup that attends adds up the weights too
 };
 // `table` (kMaxPlanSlices entries) may be null to only size the plan.
 PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table);
