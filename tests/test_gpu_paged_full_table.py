@@ -41,18 +41,18 @@ def test_append_past_the_table(dtype, ctx, new, gpu_device):
 def test_tokens_past_the_table(window, sinks, gpu_device):
     """A chunk whose last tokens have no row: every token sees of the table's positions what it would see of a longer one.  A one-token call is the last of them."""
     cap = 64
-    pages = Pages([cap] * 4, 4, 2, 64, 16, "f32", gpu_device, seed=8)
-    ctx, new = [66, 64, 90, 200], [5, 3, 40, 1]
+    pages = Pages([cap] * 5, 4, 2, 64, 16, "f32", gpu_device, seed=8)
+    ctx, new = [66, 64, 90, 200, 2 ** 31 - 1], [5, 3, 40, 1, 4]
     off = np.cumsum([0] + new).astype(np.int32)
     q = torch.randn((sum(new), 4, 64), generator=pages.generator)
     K, V, table = pages.to("K", "V", "table")
     on_gpu = lambda x: torch.as_tensor(x, dtype=torch.int32).to(gpu_device)  # noqa: E731
     got = span.paged_prompt_attn(q.to(gpu_device), K, V, table, on_gpu(ctx), on_gpu(off), 0.125, window=window, sinks=sinks).cpu().double()
     last = q[[int(o) - 1 for o in off[1:]]].contiguous().to(gpu_device)
-    weights = torch.zeros((4, 2, cap), device=gpu_device)
+    weights = torch.zeros((5, 2, cap), device=gpu_device)
     one = span.paged_decode_attn(last, K, V, table, on_gpu(ctx), 0.125, window=window, sinks=sinks, weights=weights).cpu().double()
-    sums = torch.zeros((4, 2, cap), dtype=torch.float64)
-    for b in range(4):
+    sums = torch.zeros((5, 2, cap), dtype=torch.float64)
+    for b in range(5):
         for j in range(new[b]):
             at = ctx[b] - new[b] + j
             see = [p for p in range(cap) if p <= at and (window == 0 or p > at - window or p < sinks)]
