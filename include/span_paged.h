@@ -127,6 +127,8 @@ int paged_span_decode_attn(const span_paged_desc_t* desc, const void* q, const v
  *   out : device, desc->dtype, [num_tokens, heads, head_dim]: it goes on as an activation, in the type those have
  * Scores, maxima and sums are fp32; a weight of a 16-bit call is rounded to the storage type before it meets V, as the
  * output is after it.  A token that sees nothing (more new tokens than positions) gets a row of zeros.
+ * A call is refused (SPAN_ERR_SHAPE) where num_tokens / T + min(batch, num_tokens) passes 65535, T = floor(128 / (heads / kv_heads)): with
+ * one query head per KV head 8 million tokens, with 16 524000.
  */
 int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages,
                       const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, float scale, void* out);
@@ -135,7 +137,8 @@ int paged_prompt_attn(const span_paged_desc_t* desc, const void* q, const void* 
  * Cuts every cache of more than desc->budget rows down to it, for every KV head by itself.  The rows that stay are those of
  * the first `sinks` positions, of the last `recent` (up to the largest position held), and of the others those with the
  * largest weights; of equal weights the lower slot stays, and a NaN weight counts as less than any other.  sinks + recent
- * <= budget.
+ * <= budget.  Weights are gathered by the one-token calls only: right behind a prompt they are still what they were before it, and of equal
+ * ones the first positions stay.
  * The i-th kept row in a slot from `budget` on moves to the i-th slot below it that falls free, both in ascending order, so
  * no other row is touched; the pages past the budget are the caller's again when the call's work is done.  Attention does not
  * depend on the order of the rows, but a window or a span over the slots means nothing afterwards.

@@ -130,8 +130,8 @@ PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, b
   return w;
 }
 
-// A prompt call of fewer workgroups than CUs has its tiles' positions shared out, among as many workgroups as kPromptWorkgroups allows and so that each has
-// about kPromptLeastPositions of a full table at least; a second launch joins the shares.  fp32 products take eight times as long, so that a share of two steps pays and one workgroup
+// A prompt call of fewer workgroups than CUs has its tiles' positions shared out, among as many workgroups as kPromptWorkgroups16 / 32 allow and so that each has
+// about kPromptLeastPositions16 / 32 of a full table at least; a second launch joins the shares.  fp32 products take eight times as long, so that a share of two steps pays and one workgroup
 // keeps a CU busy.  us, bf16 / fp32:
 //   never shared                 200 new of 4000, 32 heads on 8 of 128   99 /  -     64 of 3000, 8 heads of 128, fp32     - / 416
 //   256 workgroups                                                       39 /  -                                          - /  29 (64 positions at least)
