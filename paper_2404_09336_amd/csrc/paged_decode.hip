@@ -12,7 +12,7 @@
 //     and the positions are few (kPagedOwnWeights) the workgroup does that itself.
 // What bounds it: memory, and for short calls the chain of trips before the first rows and of the hand-over behind the last.  64 sequences
 // of 512 .. 4096 positions, 32 query heads on 8 KV heads of 128, bf16: 104 us, 6.0 TB/s; a window of 1024 over 32 of them, fp16: 26.7 us,
-// 5.0 TB/s; 4 of 8000 .. 32768: 55.9 us, 5.6 TB/s, with weights 67 (the scores' 10 MB cost 8 us on their way out and 5.4 in the second
+// 5.0 TB/s; 4 of 8000 .. 32768: 55.9 us, 5.6 TB/s, with weights 69 (the scores' 10 MB cost 8 us on their way out and 5.4 in the second
 // launch; stored through or past the caches they cost 4 to 7 us more); one sequence of 256 positions, fp32: 8.0 us.
 #include "paged_device.h"
 

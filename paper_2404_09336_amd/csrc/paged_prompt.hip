@@ -12,8 +12,8 @@
 // A row of K or V past the sequence's length is not read (the buffer descriptor of a page ends there) and counts as zeros.
 //
 // What bounds it: the matrix cores and, between their runs, the vector instructions of the softmax - a wave's own do not run beside its products, only the other
-// wave's of its SIMD do.  One prompt of 8192 tokens, 32 query heads on 8 KV heads of 128, bf16: 596 us, 920 TFLOP/s of the 1208 that a product of 8192^3 reaches
-// here; six chunks with a window of 1024, fp16: 188 us, 637 TFLOP/s (18 tiles a workgroup, of which 4 are cut by the window, the sinks or the diagonal).
+// wave's of its SIMD do.  One prompt of 8192 tokens, 32 query heads on 8 KV heads of 128, bf16: 597 us, 920 TFLOP/s of the 1208 that a product of 8192^3 reaches
+// here; six chunks with a window of 1024, fp16: 186 us, 643 TFLOP/s (18 tiles a workgroup, of which 4 are cut by the window, the sinks or the diagonal).
 // Tried and slower (us of those two, against 602 / 201 then): 16 query rows a wave and twice the waves 677 / 222 (twice the reads of LDS); a half tile's softmax among
 // the other half's products in one wave 661 / 223; 256 rows a workgroup whose two halves take turns 575 / 231 (faster long, slower where tiles are cut).
 #include "paged_device.h"
@@ -57,7 +57,7 @@ struct PromptShape {
   static constexpr int kKRow = kRowBytes + 16;
   // 16 bits: a row per dimension, 16-byte pieces of 8 positions, piece p of dimension d at p ^ (d / 16 % 8): 16 lanes that read a piece of 16 rows, or
   // write 8 bytes of it each for 16 units of dimensions, then meet in no bank twice.  (The 32 lanes of two quads that write side by side do, two and two: a third of the
-  // cycles that the LDS works in a long prompt are still conflicts, 51.8 of 157 million.)  fp32: a row per position, rows 4 apart half the banks apart
+  // cycles that the LDS works in a long prompt are still conflicts, 51.5 of 156 million.)  fp32: a row per position, rows 4 apart half the banks apart
   static constexpr int kVRow = kHalf ? KT * 2 + 16 : kRowBytes + 32;
   static constexpr int kKBytes = KT * kKRow, kVBytes = kHalf ? D * kVRow : KT * kVRow;
 };
