@@ -45,16 +45,18 @@ typedef struct span_paged_desc {
   int32_t num_tokens;      /* paged_append, paged_prompt_attn: rows of k_new / q                            */
   int32_t window, sinks;   /* paged_decode_attn, paged_prompt_attn: a token sees the last `window` positions up
                               to its own (0: all of them) and the first `sinks`; paged_evict: the first `sinks`
-                              positions always stay                                                         */
+                              positions always stay; paged_select: their pages are listed in any case       */
   int32_t num_intervals;   /* paged_span_decode_attn: entries held by span_starts / span_ends               */
   int32_t num_splits;      /* one-token calls: 0 = the library cuts the caches into slices as it finds best, > 0 =
                               so many slices per sequence                                                   */
-  int32_t budget, recent;  /* paged_evict                                                                   */
+  int32_t budget, recent;  /* paged_evict: rows of a cache that stay, the last of them in any case; paged_select,
+                              paged_selected_decode_attn: pages of a list; paged_select: the last positions, whose
+                              pages are listed in any case                                                  */
   const int64_t* tokens_per_seq; /* paged_span_decode_attn: HOST int64 [batch] or NULL: attended positions of every
                               sequence as span_validate returns them; they only set the slices (a wrong number costs
                               time, not correctness).  Read during the call only.                           */
-  void* workspace;         /* device, 256-byte aligned, at least paged_workspace_bytes(); for one-token calls and
-                              paged_evict its ticket counters (the first 4 * batch * (kv_heads + 1) bytes, rounded up to
+  void* workspace;         /* device, 256-byte aligned, at least paged_workspace_bytes(); for one-token calls,
+                              paged_select and paged_evict its ticket counters (the first 4 * batch * (kv_heads + 1) bytes, rounded up to
                               256) must be zero before the first call (paged_workspace_init); every call leaves them
                               zero again.  A workspace that served another batch, another number of KV heads or
                               paged_prompt_attn is initialised again.  Two calls that may overlap in time must not share one.    */
@@ -72,7 +74,11 @@ typedef enum {
   PAGED_SPAN_DECODE = 2,         /* paged_span_decode_attn                                                   */
   PAGED_SPAN_DECODE_WEIGHTS = 3, /* paged_span_decode_attn with weights                                      */
   PAGED_PROMPT = 4,              /* paged_prompt_attn                                                        */
-  PAGED_EVICT = 5                /* paged_evict                                                              */
+  PAGED_EVICT = 5,               /* paged_evict                                                              */
+  PAGED_SELECT = 16,             /* paged_select                                                             */
+  PAGED_SELECTED_DECODE = 17,    /* paged_selected_decode_attn                                               */
+  PAGED_DECODE_FP4 = 18,         /* paged_decode_attn_fp4                                                    */
+  PAGED_SPAN_DECODE_FP4 = 19     /* paged_span_decode_attn_fp4                                               */
 } span_paged_use_t;
 
 /* Bytes of workspace the call described by desc wants (0: none; also for a descriptor that would be refused). */
@@ -97,6 +103,49 @@ int paged_append(const span_paged_desc_t* desc, const void* k_new, const void* v
                  const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, int32_t* positions,
                  const int32_t* seen);
 
+/* Turns pairs of channels of a row by the angles of its token's position. */
+typedef struct paged_rotation {
+  const float* table;  /* device, 16-byte aligned, fp32 [positions, channels]: the cosines of a position's channels / 2 angles, then their sines */
+  int32_t positions;
+  int32_t channels;    /* of a row that are turned, its first ones: a multiple of 16, up to head_dim           */
+  int32_t paired;      /* 0: channel i goes with channel i + channels / 2; otherwise 2 i with 2 i + 1; i-th angle */
+} paged_rotation_t;
+
+/*
+ * paged_append with K turned on the way, and q (device, desc->dtype, [num_tokens, heads, head_dim], or NULL) into q_out (the same shape; q itself
+ * or no part of it).  The token at true position t (seen[b] - t_new + j; seen = NULL: its slot) has angles table[t]:
+ *   y_i = x_i cos - x_i' sin        y_i' = x_i sin + x_i' cos        in fp32, rounded once; channels past rotation->channels stay
+ * Where the table has no position t the turned channels become NaN.  A row of q is turned also where its row of K is dropped; rows of
+ * tokens of no sequence are left alone.
+ */
+int paged_append_rotary(const span_paged_desc_t* desc, const paged_rotation_t* rotation, const void* k_new, const void* v_new, void* k_pages,
+                        void* v_pages, const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, int32_t* positions,
+                        const int32_t* seen, const void* q, void* q_out);
+
+/*
+ * ---- a cache held in 4 bits -------------------------------------------------------------------------------
+ * The pools are uint8 [num_pages, kv_heads, page_size, head_dim / 2 + head_dim / 32]; desc->dtype is the type of the new rows, q and rows read back.
+ * A block of 32 channels of a row has an exponent e, the least from -126 on with max |x| <= 7 * 2^e, and its values are held as 2^e times the nearest
+ * of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (of two equally near the one with an even number; 7 counts as nearest to 6).  A block with a value that is not finite,
+ * or larger than 7 * 2^125, is NaN.
+ * A (page, KV head) holds page_size * head_dim / 2 bytes of codes, then page_size * head_dim / 32 of exponents (e + 127; 255: NaN).  Code: sign bit 8 and number of the value in the list;
+ * of two codes in a byte the lower channel's is the lower half.  r = row % 16 of group row / 16, c = channel:
+ *   K codes   byte  group * 8 head_dim + (c / 32) * 256 + r * 16 + c % 32 / 2
+ *   V codes   byte  group * 8 head_dim + (r / 4) * 2 head_dim + c / w * 2 w + (r % 4) * w / 2 + c % w / 2,     w = head_dim / 16
+ *   exponents byte  group * head_dim / 2 + (c / 32) * 16 + r
+ */
+
+/* paged_append into such pools, K (and q) turned on the way as by paged_append_rotary if rotation is not NULL.  K is rounded once, as if it had been turned exactly.  Without
+ * rotation q and q_out have to be NULL. */
+int paged_append_fp4(const span_paged_desc_t* desc, const paged_rotation_t* rotation, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                     const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, const int32_t* seen, const void* q, void* q_out);
+
+/* The rows that paged_append_fp4 with these lengths and offsets wrote, as values: k_rows, v_rows device, desc->dtype, [num_tokens, kv_heads, head_dim].  Rows that
+ * have no place in the cache are left as they are.  (With q_offsets over whole sequences: a cache as paged_append takes it, for paged_prompt_attn.  A value that
+ * fp16 does not hold becomes infinite there.) */
+int paged_read_fp4(const span_paged_desc_t* desc, const void* k_pages, const void* v_pages, const int32_t* block_table, const int32_t* ctx_lens,
+                   const int32_t* q_offsets, void* k_rows, void* v_rows);
+
 /*
  * Attention of one new token per sequence (its row already appended) over S_b, the positions
  *   max(0, n - window) <= p < n  (all p < n for window 0)  and  p < min(sinks, n),      n = ctx_lens[b],
@@ -119,6 +168,37 @@ int paged_decode_attn(const span_paged_desc_t* desc, const void* q, const void* 
 int paged_span_decode_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages,
                            const int32_t* block_table, const int32_t* span_offsets, const int32_t* span_starts,
                            const int32_t* span_ends, float scale, float* weights, float* out);
+
+/* Both over a cache held in 4 bits, without weights. */
+int paged_decode_attn_fp4(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                          const int32_t* ctx_lens, float scale, float* out);
+int paged_span_decode_attn_fp4(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                               const int32_t* span_offsets, const int32_t* span_starts, const int32_t* span_ends, float scale, float* out);
+
+/*
+ * Which pages of a sequence a token's queries may find most in, for every KV head by itself.  bounds holds the least and the largest value of every channel
+ * over a page's rows of K; a page's score is an upper bound of what the group's queries can score with one of its rows, added up over them:
+ *   score_j = sum over d of  max_part_d * hi[j, d] + min_part_d * lo[j, d]     max_part_d = sum over the group of max(q_d, 0), min_part_d of min(q_d, 0)
+ * in 64 bits, rounded to 32.  Listed are the pages of the first desc->sinks and of the last max(desc->recent, 1) positions and those that score highest of the
+ * others, desc->budget at most, all where there are no more; of equal scores the lower page, NaN ahead of any number, a page outside the pool with a score
+ * of minus infinity.  What the protected positions can lie on has to fit: ceil(sinks / page_size) + floor((max(recent, 1) + page_size - 2) / page_size) + 1 <= budget.
+ *   q        : device, desc->dtype, [batch, heads, head_dim], turned as K is
+ *   bounds   : device, desc->dtype, [num_pages, kv_heads, 2, head_dim] (least, largest): read, and written where rows are new
+ *   since    : device int32 [batch] or NULL (ctx_lens - 1): positions from here on are new.  The bounds of their pages are made on the way, from the new rows and,
+ *              where a page begins ahead of since[b], what its bounds are already.  0 after a prompt, or after rows moved
+ *   selected : device int32 [batch, kv_heads, budget]: page numbers within the sequence (columns of block_table), ascending, then -1
+ * Pages written to must belong to one sequence only.  A NaN in a new row makes its page's bounds NaN.
+ */
+int paged_select(const span_paged_desc_t* desc, const void* q, const void* k_pages, void* bounds, const int32_t* block_table, const int32_t* ctx_lens,
+                 const int32_t* since, int32_t* selected);
+
+/*
+ * paged_decode_attn over the listed pages: S of (b, KV head) is the positions p < ctx_lens[b] on pages selected[b, h, i], i < desc->budget.  Entries outside
+ * [0, table_pages) attend nothing; of a sequence of c pages the first min(c, budget) entries are looked at, which should differ from one another (a
+ * page listed twice counts twice).
+ */
+int paged_selected_decode_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                               const int32_t* ctx_lens, const int32_t* selected, float scale, float* out);
 
 /*
  * Attention of all new tokens of every sequence (their rows already appended): a prompt, or a chunk of one behind a cached

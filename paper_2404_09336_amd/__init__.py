@@ -15,5 +15,8 @@ from .binding import (  # noqa: F401
 from .paged import (  # noqa: F401
     paged_append, prepare_paged_append, paged_decode_attn, prepare_paged_decode_attn,
     paged_span_decode_attn, prepare_paged_span_decode_attn, paged_prompt_attn, prepare_paged_prompt_attn, paged_evict, prepare_paged_evict,
+    paged_append_rotary, prepare_paged_append_rotary, paged_append_fp4, prepare_paged_append_fp4, paged_read_fp4, prepare_paged_read_fp4,
+    paged_decode_attn_fp4, prepare_paged_decode_attn_fp4, paged_span_decode_attn_fp4, prepare_paged_span_decode_attn_fp4,
+    paged_select, prepare_paged_select, paged_selected_decode_attn, prepare_paged_selected_decode_attn, fp4_pages,
     paged_workspace_bytes, paged_workspace_init,
 )

@@ -14,6 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspanattn.so")
 SOURCES = [os.path.join(CSRC, name) for name in ("span_kernels.hip", "span_matrix.hip", "paged_decode.hip", "paged_cache.hip", "paged_prompt.hip",
+                                                 "paged_append.hip", "paged_fp4.hip", "paged_select.hip",
                                                  "span_host.cpp", "paged_host.cpp")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          # keep the compiler from forming packed-fp32 instructions

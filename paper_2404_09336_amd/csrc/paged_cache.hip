@@ -24,21 +24,6 @@ struct AppendArgs {
 
 constexpr int kAppendLoads = 4;  // pieces of K and of V per lane: a wave moves up to 4 KB of each
 
-// The first sequence that ends behind row t, by sixty-fourths of the list: one load per step, one step for up to 64 sequences.
-// Returns -1 where there is none.
-__device__ __forceinline__ int sequence_of(const int32_t* offsets, int batch, int t, int lane) {
-  int low = 0, n = batch;
-  while (true) {
-    const int step = (n + 63) >> 6;
-    const bool ended = offsets[low + min((lane + 1) * step, n)] <= t;
-    const int past = __popcll(__builtin_amdgcn_ballot_w64(ended)) * step;
-    if (past >= n) return -1;
-    low += past;
-    if (step == 1) return low;
-    n = min(step, n - past);
-  }
-}
-
 // A wave takes 4 KB of one token's rows.  The rows themselves are asked for first; meanwhile the sequence is found and its page.  Prompts of 16 sequences
 // (20600 rows of 32 heads of 128, bf16) take 126 us, 5.35 TB/s read and written, which is what a large copy reaches; 64 rows of a step 3.4 us, a launch's least.
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {

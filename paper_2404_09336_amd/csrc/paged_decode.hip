@@ -14,35 +14,13 @@
 // of 512 .. 4096 positions, 32 query heads on 8 KV heads of 128, bf16: 104 us, 6.0 TB/s; a window of 1024 over 32 of them, fp16: 26.7 us,
 // 5.0 TB/s; 4 of 8000 .. 32768: 55.9 us, 5.6 TB/s, with weights 69 (the scores' 10 MB cost 8 us on their way out and 5.4 in the second
 // launch; stored through or past the caches they cost 4 to 7 us more); one sequence of 256 positions, fp32: 8.0 us.
-#include "paged_device.h"
+#include "paged_attend.h"
 
 namespace spanattn {
 
 namespace {
 
 constexpr int kPWin = 512;  // rows of a wave whose pool rows are tabulated at a time
-
-struct PagedArgs : LaunchArgs {  // heads: KV heads; max_len: positions of a sequence's table; k, v: the pools
-  const int32_t* block_table;
-  int32_t table_pages, page_shift, num_pages;
-  int32_t group;             // query heads per KV head
-  int32_t batch, window, sinks;
-  int32_t room, more_room;   // > 0: slices per head aimed at, see locate_slice; 0: num_splits each, or the table
-  int32_t whole;             // up to so many positions a sequence is not cut
-  float* scores;             // [batch, kv head, query head of the group, max_len] unscaled scores by virtual position, or null
-  float* final_ml;           // [batch, query head] (maximum, sum)
-  int32_t* counts;           // span form with weights: [batch] attended positions
-  int32_t* list;             // ... and [batch, max_len] the positions themselves
-  float* weights;
-  int32_t weights_here;      // 1: the workgroup that attends adds up the weights too (PagedPlan::own_weights)
-};
-struct PagedArgsPlain : PagedArgs {
-  static constexpr bool kHasTable = false;
-};
-struct PagedArgsTable : PagedArgs {
-  static constexpr bool kHasTable = true;
-  uint32_t table[kMaxPlanSlices];  // pack_slice entries
-};
 
 template <class Elt, int D>
 struct PagedShape {
@@ -55,75 +33,6 @@ struct PagedShape {
   static constexpr int S = kRowBytes == 128 ? 2 : 1;
   static constexpr int kWaves = kRowBytes == 512 ? 2 : 4;  // per SIMD
 };
-
-struct Slice {
-  int b, split, nsl, y0, len;  // sequence, slice within it, slices of it, slot of its first slice; its length (locate_slice)
-};
-
-// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than `whole`, T whole steps and
-// kPagedLeastSlice at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
-// many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice well above the
-// mean, which is what the whole call waits for then, `more_room` is tried.  Every workgroup works it out for itself: one load of the lengths,
-// which it needs anyway, and a few scans for up to 64 sequences.
-// (us, 1024 workgroups always -> 512 and 1024 where those are not level: 32 sequences in a window of 1024 29.0 -> 27.0, four of 8000 .. 32768 72.9 -> 68.7;
-// 512 always: 64 x 8 pairs of 512 .. 4096 106.4 -> 112.2.  One round each way: with as many slices as came out, 1.25 rounds, those took 110.9.)
-__device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lane) {
-  int len = 0, n = 0;
-  auto fetch = [&](int c) {
-    len = c + lane < a.batch ? a.ctx_lens[c + lane] : 0;
-    n = seen_by_last(len, a.max_len, a.window, a.sinks).count;
-  };
-  uint32_t all = 0, longest = 1;
-  for (int c = 0; c < a.batch; c += 64) {
-    fetch(c);
-    all += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(n), 63);
-    longest = max(longest, (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_max(n), 63));
-  }
-  auto steps = [](uint32_t x) { return (x + kPagedSliceStep - 1u) / kPagedSliceStep * kPagedSliceStep; };
-  auto slices = [&](uint32_t T) { return n > a.whole ? (int)(((uint32_t)n + T - 1u) / T) : 1; };  // of this lane's sequence
-  const uint32_t batch = (uint32_t)a.batch;
-  uint32_t T = longest;
-  if (longest > (uint32_t)a.whole) {
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-      const uint32_t room = (uint32_t)(pass == 0 ? a.room : a.more_room);
-      T = longest;
-      if (room > batch) {
-        const float mean = (float)all / ((float)room - 0.5f * (float)batch);  // (a sequence has half a slice more than its share on average)
-        T = max(steps((uint32_t)mean), (uint32_t)kPagedLeastSlice);
-        while (T < longest) {
-          uint32_t total = 0;
-          for (int c = 0; c < a.batch; c += 64) {
-            if (a.batch > 64) fetch(c);
-            total += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(c + lane < a.batch ? slices(T) : 0), 63);
-          }
-          if (total <= room) break;
-          T = min(max(steps((uint32_t)((float)T * (float)total / (float)room)), steps(T + T / 16)), longest);
-        }
-      }
-      if ((float)min(T, longest) * (float)max(room, batch) <= 1.4f * (float)all || T <= (uint32_t)kPagedLeastSlice) break;
-    }
-  }
-  Slice s = {-1, 0, 1, 0, 0};
-  int before = 0;
-  for (int c = 0; c < a.batch; c += 64) {
-    if (a.batch > 64) fetch(c);
-    const int nsl = c + lane < a.batch ? slices(T) : 0;
-    const int incl = before + wave_inclusive_scan(nsl);
-    const uint64_t past = __builtin_amdgcn_ballot_w64(incl > y);
-    if (past != 0) {
-      const int at = (int)__builtin_ctzll(past);
-      s.b = c + at;
-      s.nsl = __builtin_amdgcn_readlane(nsl, at);
-      s.y0 = __builtin_amdgcn_readlane(incl, at) - s.nsl;
-      s.split = y - s.y0;
-      s.len = __builtin_amdgcn_readlane(len, at);
-      break;
-    }
-    before = __builtin_amdgcn_readlane(incl, 63);
-  }
-  return s;
-}
 
 // weights[b, h, p] += sum over the group's heads of exp2((score - maximum) * post) / sum, for the positions with virtual numbers v0 .. v0 + 3.  A
 // position is one thread's, so the sums do not depend on any order.
@@ -152,22 +61,13 @@ __device__ __forceinline__ void add_weights(const PagedArgs& a, const Seen& seen
   }
 }
 
-// A wave's instruction priority falls as it gets on with its rows.  Among equals a SIMD issues the oldest wave first, and the workgroups that arrive last on
-// a CU got their first rows when the others were nearly done (stamps: after 5 to 67 us of a call of 107), to end alone.  64 x 8 pairs of 512 .. 4096
-// 107.1 -> 104.6; smaller calls 0 to 1 %.
-__device__ __forceinline__ void priority(int done, int quarter) {
-  if (done == 0) __builtin_amdgcn_s_setprio(3);
-  else if (done == quarter) __builtin_amdgcn_s_setprio(2);
-  else if (done == 2 * quarter) __builtin_amdgcn_s_setprio(1);
-  else if (done == 3 * quarter) __builtin_amdgcn_s_setprio(0);
-}
-
 // kWeights: a call that adds up weights.  (Code that is jumped over is fetched all the same: without weights the few microseconds of the smallest calls
 // are 0.3 to 0.7 shorter for its absence.)
-template <class Elt, int D, bool kSpans, bool kWeights, class Args>
+template <class Elt, int D, PagedKind kKind, bool kWeights, class Args>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D>::kWaves))) void paged_kernel(const Args a) {
   using Shape = PagedShape<Elt, D>;
+  constexpr bool kSpans = kKind == kPagedSpans, kSelected = kKind == kPagedSelected;
   constexpr int NK = Shape::NK, NE = Shape::NE, VW = Shape::VW, S = Shape::S;
   constexpr int TR = 16 * S;  // rows of a step
   constexpr uint32_t ROWB = Shape::kRowBytes;
@@ -209,7 +109,9 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     sl = Slice{(int)(entry & 1023u), (int)(entry >> 10 & 2047u), (int)(entry >> 21), 0, 0};
     sl.y0 = (int)blockIdx.y - sl.split;
   } else if (!kSpans && a.room > 0) {
-    sl = locate_slice(a, (int)blockIdx.y, lane);
+    sl = locate_slice(a, (int)blockIdx.y, lane, [&](int len) {
+      return kSelected ? selected_positions(a, len) : seen_by_last(len, a.max_len, a.window, a.sinks).count;
+    });
     if (sl.b < 0) return;  // (the grid holds the most slices that any lengths give)
   } else {
     sl.nsl = a.num_splits;
@@ -245,8 +147,12 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     n_total = clampi(count_positions(a, intervals, wave, lane, s_u.st.tab), 0, a.max_len);
   } else {
     if (a.room == 0) sl.len = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]);
-    seen = seen_by_last(sl.len, a.max_len, a.window, a.sinks);
-    n_total = seen.count;
+    if constexpr (kSelected) {
+      n_total = selected_positions(a, sl.len);
+    } else {
+      seen = seen_by_last(sl.len, a.max_len, a.window, a.sinks);
+      n_total = seen.count;
+    }
   }
   n_total = __builtin_amdgcn_readfirstlane(n_total);
   // even shares of whole steps
@@ -278,8 +184,9 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
         const int v = vrow(w0 + r);
         int p;
         if constexpr (kSpans) p = clampi(s_row[wave][r], 0, a.max_len - 1);  // (a list whose positions add up past 32 bits leaves rows that the walk does not find)
+        else if constexpr (kSelected) p = selected_position(a, bh, sl.len, v);
         else p = v < seen.sinks ? v : v - seen.sinks + seen.low;
-        x = pool_row(table, p, a.page_shift, a.num_pages);
+        if (!kSelected || p >= 0) x = pool_row(table, p, a.page_shift, a.num_pages);
         // (who adds up weights reads his own entries back; the heads' are equal)
         if (kSpans && kWeights && (h == 0 || a.weights_here)) a.list[(size_t)b * a.max_len + v] = p;
       }
@@ -551,128 +458,13 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
     add_outputs(sc, cur);
   }
 
-  // ---- the waves' states are merged in LDS -------------------------------------------------------------
+  // ---- the waves' states, and the slices', are merged --------------------------------------------------
   lsum = across_groups_sum<16>(lsum) * Elt::kWeightScale;
-  if (c4 == 0) s_ml[qi][wave] = f32x2{ref, lsum};
-  constexpr int kPerToken = kThreads / 16, kQuads = D / 4 / kPerToken;
-  const int mine = tid / kPerToken, part = tid % kPerToken;  // query head, share of its quads of columns
-  const bool direct = nsl == 1;
-  const size_t slot0 = (size_t)sl.y0 * kv_heads + h, my_slot = slot0 + (size_t)split * kv_heads;
-  auto acc_slot = [&](size_t slot) { return slab_resource(a.part_acc + slot * (size_t)(group * D), (uint32_t)(group * D) * 4u); };
-  auto ml_slot = [&](size_t slot) { return slab_resource(a.part_ml + slot * (size_t)(group * 2), (uint32_t)group * 8u); };
-  auto store_row = [&](float M, float L, const f32x4 (&o)[kQuads]) {
-    const float sum = L != 0.f ? L : 1.f;
-    float* row = a.out + qrow(mine) * D + 4 * part;
-#pragma unroll
-    for (int i = 0; i < kQuads; ++i) *reinterpret_cast<f32x4*>(row + 4 * kPerToken * i) = f32x4{o[i][0] / sum, o[i][1] / sum, o[i][2] / sum, o[i][3] / sum};
-    if (kWeights && part == 0) *reinterpret_cast<f32x2*>(a.final_ml + 2 * qrow(mine)) = f32x2{M, L / Elt::kWeightScale};
-  };
-  __syncthreads();  // the (maximum, sum) pairs are in LDS; the streaming tables are no longer read
-  if (qi < group) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-#pragma unroll
-      for (int u = 0; u < NE / 4; ++u)
-        *reinterpret_cast<f32x4*>(&s_u.ws.acc[wave][qi][column(4 * c4 + r, u)]) = f32x4{O[4 * u][r], O[4 * u + 1][r], O[4 * u + 2][r], O[4 * u + 3][r]};
-    }
+  const bool whole = finish_pair<D, NE, kSplitPieces, kWeights>(a, sl, h, ref, lsum, O, post, Elt::kWeightScale, s_ml, s_u.ws.acc, s_ticket);
+  if (kWeights && whole && a.weights_here) {  // (no sequence of the call is cut: nothing else is waited for)
+    __syncthreads();                          // scores, list and final states are written
+    for (int v0 = 4 * tid; v0 < n_total; v0 += 4 * kThreads) add_weights<Elt, kSpans>(a, seen, n_total, b, h, v0);
   }
-  float weight[kWavesPerBlock], M = -INFINITY, L = 0.f;
-  {
-    f32x2 ml[kWavesPerBlock];
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w) ml[w] = s_ml[mine][w];
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w)
-      if (ml[w][1] != 0.f) M = fmaxf(M, ml[w][0]);  // (a NaN sum counts: it has to reach the output)
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w) {
-      weight[w] = ml[w][1] != 0.f ? __builtin_amdgcn_exp2f((ml[w][0] - M) * post) : 0.f;
-      L = fmaf(weight[w], ml[w][1], L);
-    }
-  }
-  __syncthreads();
-  if (mine < group) {
-    f32x4 o[kQuads];
-#pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-      o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < kWavesPerBlock; ++w) {
-        const f32x4 ow = *reinterpret_cast<const f32x4*>(&s_u.ws.acc[w][mine][4 * (part + kPerToken * i)]);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[i][k] = fmaf(weight[w], ow[k], o[i][k]);
-      }
-    }
-    if (direct) {
-      store_row(M, L, o);
-    } else {
-      const __amdgpu_buffer_rsrc_t slot = acc_slot(my_slot);
-#pragma unroll
-      for (int i = 0; i < kQuads; ++i) publish4(slot, (uint32_t)(mine * D + 4 * (part + kPerToken * i)) * 4u, o[i]);
-      if (part == 0) __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{M, L}), ml_slot(my_slot), (uint32_t)mine * 8u, 0, kThrough);
-    }
-  }
-  if (direct) {
-    if (kWeights && a.weights_here) {  // (no sequence of the call is cut: nothing else is waited for)
-      __syncthreads();     // scores, list and final states are written
-      for (int v0 = 4 * tid; v0 < n_total; v0 += 4 * kThreads) add_weights<Elt, kSpans>(a, seen, n_total, b, h, v0);
-    }
-    return;
-  }
-
-  // ---- several slices: the workgroup that arrives last for the pair merges them all (the hand-over of matrix_kernel) ----
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // my published stores are acknowledged
-  __syncthreads();
-  if (tid == 0) s_ticket = (uint32_t)__hip_atomic_fetch_add(a.counters + bh * (size_t)a.counter_stride, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __syncthreads();
-  if (s_ticket != (uint32_t)(nsl - 1)) return;
-  if (mine < group) {
-    constexpr int kMerge = 8;
-    f32x4 o[kQuads];
-#pragma unroll
-    for (int i = 0; i < kQuads; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    M = -INFINITY;
-    L = 0.f;
-    for (int s0 = 0; s0 < nsl; s0 += kMerge) {
-      f32x2 ml[kMerge];
-      f32x4 os[kMerge][kQuads];
-#pragma unroll
-      for (int k = 0; k < kMerge; ++k) {
-        const size_t slot = slot0 + (size_t)min(s0 + k, nsl - 1) * kv_heads;  // (past the end: a slot that exists, unused)
-        ml[k] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(ml_slot(slot), (uint32_t)mine * 8u, 0, kThrough));
-        const __amdgpu_buffer_rsrc_t states = acc_slot(slot);
-#pragma unroll
-        for (int i = 0; i < kQuads; ++i) os[k][i] = observe4(states, (uint32_t)(mine * D + 4 * (part + kPerToken * i)) * 4u);
-      }
-      const float before = M;
-#pragma unroll
-      for (int k = 0; k < kMerge; ++k) {
-        if (s0 + k >= nsl) ml[k][1] = 0.f;
-        if (ml[k][1] != 0.f) M = fmaxf(M, ml[k][0]);
-      }
-      const float safe = M == -INFINITY ? 0.f : M;
-      if (s0 > 0) {
-        const float old = __builtin_amdgcn_exp2f((before - safe) * post);
-        L *= old;
-#pragma unroll
-        for (int i = 0; i < kQuads; ++i) o[i] *= old;
-      }
-#pragma unroll
-      for (int k = 0; k < kMerge; ++k) {
-        if (s0 + k < nsl) {
-          const float w = ml[k][1] != 0.f ? __builtin_amdgcn_exp2f((ml[k][0] - safe) * post) : 0.f;
-          L = fmaf(w, ml[k][1], L);
-#pragma unroll
-          for (int i = 0; i < kQuads; ++i) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[i][c] = fmaf(w, os[k][i][c], o[i][c]);
-          }
-        }
-      }
-    }
-    store_row(M, L, o);
-  }
-  if (tid == 0) __hip_atomic_store(a.counters + bh * (size_t)a.counter_stride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 template <class Elt, bool kSpans>
@@ -695,17 +487,22 @@ __global__ __launch_bounds__(256) void clear_words_kernel(uint32_t* p, size_t n)
 }
 
 
-template <class Elt, int D, bool kSpans>
+template <class Elt, int D, PagedKind kKind>
 int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, hipStream_t stream) {
   const dim3 grid((unsigned)base.heads, (unsigned)p.rows);
   auto start = [&](const auto& a) {
     using Args = std::decay_t<decltype(a)>;
-    if (a.weights != nullptr) hipLaunchKernelGGL((paged_kernel<Elt, D, kSpans, true, Args>), grid, dim3(kThreads), 0, stream, a);
-    else hipLaunchKernelGGL((paged_kernel<Elt, D, kSpans, false, Args>), grid, dim3(kThreads), 0, stream, a);
+    if constexpr (kKind != kPagedSelected) {
+      if (a.weights != nullptr) {
+        hipLaunchKernelGGL((paged_kernel<Elt, D, kKind, true, Args>), grid, dim3(kThreads), 0, stream, a);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((paged_kernel<Elt, D, kKind, false, Args>), grid, dim3(kThreads), 0, stream, a);
   };
   PagedArgsPlain plain;
   static_cast<PagedArgs&>(plain) = base;
-  if constexpr (kSpans) {  // (dense calls find their slices on the device)
+  if constexpr (kKind == kPagedSpans) {  // (the others find their slices on the device)
     if (p.table) {
       PagedArgsTable a;
       static_cast<PagedArgs&>(a) = base;
@@ -720,68 +517,29 @@ int run_paged(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, 
   const int rc = launched();
   if (rc != SPAN_OK || base.weights == nullptr || base.weights_here) return rc;
   int64_t most = base.max_len;
-  if (!kSpans && base.window > 0 && (int64_t)base.window + base.sinks < most) most = (int64_t)base.window + base.sinks;
-  hipLaunchKernelGGL((weights_kernel<Elt, kSpans>), dim3((unsigned)((most + 1023) / 1024), (unsigned)base.heads, (unsigned)base.batch), dim3(256), 0,
+  if (kKind == kPagedDense && base.window > 0 && (int64_t)base.window + base.sinks < most) most = (int64_t)base.window + base.sinks;
+  hipLaunchKernelGGL((weights_kernel<Elt, kKind == kPagedSpans>), dim3((unsigned)((most + 1023) / 1024), (unsigned)base.heads, (unsigned)base.batch), dim3(256), 0,
                      stream, base);
   return launched();
 }
 
-template <bool kSpans>
+template <PagedKind kKind>
 int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const void* v, const int32_t* block_table, const int32_t* ctx_lens,
-                 const int32_t* offsets, const int32_t* starts, const int32_t* ends, float scale, float* weights, float* out) {
-  const int rc = check_paged(d);
-  if (rc != SPAN_OK) return rc;
-  if (!q || !k || !v || !block_table || !out) return SPAN_ERR_NULL;
-  if (kSpans ? !offsets || (d->num_intervals > 0 && (!starts || !ends)) : !ctx_lens) return SPAN_ERR_NULL;
+                 const int32_t* offsets, const int32_t* starts, const int32_t* ends, const int32_t* selected, float scale, float* weights, float* out) {
+  PagedArgs a;
+  PagedPlan p;
   uint32_t table[kMaxPlanSlices];
-  const PagedPlan p = plan_paged(d, kSpans, table);
-  const PagedWorkspace w = paged_workspace(d, p, kSpans, weights != nullptr);
-  if (w.total > 0 && (!d->workspace || ((uintptr_t)d->workspace & 255u) || d->workspace_bytes < w.total)) return SPAN_ERR_WORKSPACE;
-  char* at = (char*)d->workspace;
-  PagedArgs a = {};
-  a.q = q;
-  a.k = k;
-  a.v = v;
-  a.out = out;
-  a.offsets = offsets;
-  a.starts = starts;
-  a.ends = ends;
-  a.ctx_lens = ctx_lens;
-  a.counters = w.sliced ? (int32_t*)at : nullptr;
-  a.counter_stride = (int32_t)(counter_bytes(d) / sizeof(int32_t) / ((size_t)d->batch * d->kv_heads));
-  a.part_ml = w.sliced ? (float*)(at + w.ml) : nullptr;
-  a.part_acc = w.sliced ? (float*)(at + w.acc) : nullptr;
-  a.heads = d->kv_heads;
-  a.max_len = a.max_tokens = capacity(d);
-  a.num_intervals = d->num_intervals;
-  a.num_splits = p.cut ? p.splits : 1;
-  a.scale_log2e = scale * 1.4426950408889634f;
-  a.block_table = block_table;
-  a.table_pages = d->table_pages;
-  a.page_shift = page_shift(d);
-  a.num_pages = d->num_pages;
-  a.group = d->heads / d->kv_heads;
-  a.batch = d->batch;
-  a.window = d->window;
-  a.sinks = d->sinks;
-  a.room = p.cut ? p.room : 0;
-  a.more_room = p.rows;
-  a.whole = paged_whole(d);
-  a.final_ml = weights ? (float*)(at + w.final_ml) : nullptr;
-  a.counts = weights && kSpans ? (int32_t*)(at + w.counts) : nullptr;
-  a.list = weights && kSpans ? (int32_t*)(at + w.list) : nullptr;
-  a.scores = weights ? (float*)(at + w.scores) : nullptr;
-  a.weights = weights;
-  a.weights_here = weights && p.own_weights ? 1 : 0;
+  const int rc = one_token_args(d, kKind, q, k, v, block_table, ctx_lens, offsets, starts, ends, selected, scale, weights, out, &a, &p, table);
+  if (rc != SPAN_OK) return rc;
   hipStream_t stream = (hipStream_t)d->stream;
   const bool d128 = d->head_dim == 128;
   switch (d->dtype) {
     case SPAN_F32:
-      return d128 ? run_paged<F32, 128, kSpans>(a, p, table, stream) : run_paged<F32, 64, kSpans>(a, p, table, stream);
+      return d128 ? run_paged<F32, 128, kKind>(a, p, table, stream) : run_paged<F32, 64, kKind>(a, p, table, stream);
     case SPAN_F16:
-      return d128 ? run_paged<F16, 128, kSpans>(a, p, table, stream) : run_paged<F16, 64, kSpans>(a, p, table, stream);
+      return d128 ? run_paged<F16, 128, kKind>(a, p, table, stream) : run_paged<F16, 64, kKind>(a, p, table, stream);
     default:
-      return d128 ? run_paged<BF16, 128, kSpans>(a, p, table, stream) : run_paged<BF16, 64, kSpans>(a, p, table, stream);
+      return d128 ? run_paged<BF16, 128, kKind>(a, p, table, stream) : run_paged<BF16, 64, kKind>(a, p, table, stream);
   }
 }
 
@@ -790,13 +548,20 @@ int paged_decode(const span_paged_desc_t* d, const void* q, const void* k, const
 
 extern "C" int paged_decode_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
                                  const int32_t* ctx_lens, float scale, float* weights, float* out) {
-  return spanattn::paged_decode<false>(desc, q, k_pages, v_pages, block_table, ctx_lens, nullptr, nullptr, nullptr, scale, weights, out);
+  return spanattn::paged_decode<spanattn::kPagedDense>(desc, q, k_pages, v_pages, block_table, ctx_lens, nullptr, nullptr, nullptr, nullptr, scale, weights, out);
 }
 
 extern "C" int paged_span_decode_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages,
                                       const int32_t* block_table, const int32_t* span_offsets, const int32_t* span_starts,
                                       const int32_t* span_ends, float scale, float* weights, float* out) {
-  return spanattn::paged_decode<true>(desc, q, k_pages, v_pages, block_table, nullptr, span_offsets, span_starts, span_ends, scale, weights, out);
+  return spanattn::paged_decode<spanattn::kPagedSpans>(desc, q, k_pages, v_pages, block_table, nullptr, span_offsets, span_starts, span_ends, nullptr, scale,
+                                                       weights, out);
+}
+
+extern "C" int paged_selected_decode_attn(const span_paged_desc_t* desc, const void* q, const void* k_pages, const void* v_pages,
+                                          const int32_t* block_table, const int32_t* ctx_lens, const int32_t* selected, float scale, float* out) {
+  return spanattn::paged_decode<spanattn::kPagedSelected>(desc, q, k_pages, v_pages, block_table, ctx_lens, nullptr, nullptr, nullptr, selected, scale,
+                                                          nullptr, out);
 }
 
 extern "C" int paged_workspace_init(const span_paged_desc_t* desc) {

@@ -27,6 +27,21 @@ __device__ __forceinline__ int pool_row(const int32_t* table_of_b, int p, int pa
   return (uint32_t)page < (uint32_t)num_pages ? (page << page_shift) + (p & ((1 << page_shift) - 1)) : -1;
 }
 
+// The first sequence that ends behind row t, by sixty-fourths of the list: one load per step, one step for up to 64 sequences.
+// Returns -1 where there is none.
+__device__ __forceinline__ int sequence_of(const int32_t* offsets, int batch, int t, int lane) {
+  int low = 0, n = batch;
+  while (true) {
+    const int step = (n + 63) >> 6;
+    const bool ended = offsets[low + min((lane + 1) * step, n)] <= t;
+    const int past = __popcll(__builtin_amdgcn_ballot_w64(ended)) * step;
+    if (past >= n) return -1;
+    low += past;
+    if (step == 1) return low;
+    n = min(step, n - past);
+  }
+}
+
 // Positions that the token at position n - 1 sees: [0, sinks) and from `low` on, of those below n that the table has.
 struct Seen {
   int sinks, low, count;

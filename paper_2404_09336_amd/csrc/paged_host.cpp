@@ -34,7 +34,7 @@ constexpr int64_t kPagedWorkgroups = 512, kPagedMoreWorkgroups = 1024;
 // heads each, 115.5 -> 110.7.
 constexpr int64_t kPagedOwnWeights = 3 << 19;
 
-PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
+PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table) {
   PagedPlan p = {0, 1, false, 0, false, false};
   const int64_t cap = capacity(d), whole = paged_whole(d);
   const int64_t room = std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads), more_room = std::max<int64_t>(1, kPagedMoreWorkgroups / d->kv_heads);
@@ -48,9 +48,11 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
     return p;
   };
   if (d->num_splits > 0) return uniform(d->num_splits);
-  if (!spans) {
+  if (kind != kPagedSpans) {
     if (d->batch > kPagedLocateBatch) return uniform(1);
-    const int64_t most = d->window > 0 ? std::min<int64_t>(cap, (int64_t)d->window + d->sinks) : cap;  // positions of any sequence
+    int64_t most = cap;  // positions of any sequence
+    if (kind == kPagedSelected) most = std::min<int64_t>(cap, (int64_t)d->budget * d->page_size);
+    else if (d->window > 0) most = std::min<int64_t>(cap, (int64_t)d->window + d->sinks);
     if (most <= whole) return uniform(1);
     p.room = (int32_t)room;
     p.splits = 2;
@@ -107,7 +109,8 @@ PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) {
   return uniform(std::min(ceil_div(room, d->batch), ceil_div(cap, kPagedLeastSlice)));
 }
 
-PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights) {
+PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, PagedKind kind, bool weights) {
+  const bool spans = kind == kPagedSpans;
   PagedWorkspace w = {};
   w.sliced = p.splits > 1;
   w.weights = weights;
@@ -177,6 +180,24 @@ size_t evict_workspace(const span_paged_desc_t* d) {
   return (counter_bytes(d) + lists + 255) & ~(size_t)255;
 }
 
+int check_rotation(const span_paged_desc_t* d, const paged_rotation_t* r) {
+  if (!r) return SPAN_OK;
+  if (!r->table) return SPAN_ERR_NULL;
+  if ((uintptr_t)r->table & 15u) return SPAN_ERR_SHAPE;
+  if (r->positions <= 0 || r->channels <= 0 || r->channels % 16 != 0 || r->channels > d->head_dim) return SPAN_ERR_SHAPE;
+  return SPAN_OK;
+}
+
+// Pages that the first `sinks` and the last `recent` positions can lie on have to fit the list.
+int check_select(const span_paged_desc_t* d) {
+  const int64_t first = ceil_div(d->sinks, d->page_size), last = (std::max<int64_t>(d->recent, 1) + d->page_size - 2) / d->page_size + 1;
+  return d->budget < 1 || first + last > d->budget ? SPAN_ERR_SHAPE : SPAN_OK;
+}
+
+size_t select_workspace(const span_paged_desc_t* d) {
+  return counter_bytes(d) + (((size_t)d->batch * d->kv_heads * (size_t)d->table_pages * sizeof(float) + 255) & ~(size_t)255);
+}
+
 }  // namespace spanattn
 
 extern "C" int paged_check(const span_paged_desc_t* desc) { return spanattn::check_paged(desc); }
@@ -186,6 +207,12 @@ extern "C" size_t paged_workspace_bytes(const span_paged_desc_t* desc, int use) 
   if (check_paged(desc) != SPAN_OK) return 0;
   if (use == PAGED_EVICT) return evict_workspace(desc);
   if (use == PAGED_PROMPT) return prompt_workspace(desc, plan_prompt(desc));
+  if (use == PAGED_SELECT) return check_select(desc) == SPAN_OK ? select_workspace(desc) : 0;
+  if (use == PAGED_SELECTED_DECODE && desc->budget < 1) return 0;
+  if (use >= PAGED_SELECTED_DECODE && use <= PAGED_SPAN_DECODE_FP4) {
+    const PagedKind kind = use == PAGED_SELECTED_DECODE ? kPagedSelected : use == PAGED_DECODE_FP4 ? kPagedDense : kPagedSpans;
+    return paged_workspace(desc, plan_paged(desc, kind, nullptr), kind, false).total;
+  }
   if (use < PAGED_DECODE || use > PAGED_SPAN_DECODE_WEIGHTS) return 0;
   const bool spans = use >= PAGED_SPAN_DECODE;
   return paged_workspace(desc, plan_paged(desc, spans, nullptr), spans, (use & 1) != 0).total;

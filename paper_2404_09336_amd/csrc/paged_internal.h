@@ -25,6 +25,9 @@ inline size_t counter_bytes(const span_paged_desc_t* d) { return ((size_t)d->bat
 inline int page_shift(const span_paged_desc_t* d) { return __builtin_ctz((unsigned)d->page_size); }
 inline int32_t capacity(const span_paged_desc_t* d) { return d->table_pages * d->page_size; }  // positions of a sequence's table
 
+// What a one-token call attends: the cache up to a token (window, sinks), a sequence's span, or the pages listed for a (sequence, KV head).
+enum PagedKind { kPagedDense, kPagedSpans, kPagedSelected };
+
 // How a one-token call is cut.
 struct PagedPlan {
   int32_t room;      // > 0: slices per head the kernel aims at over all sequences (locate_slice; `rows` where that is not level)
@@ -35,14 +38,18 @@ struct PagedPlan {
   bool own_weights;  // the workgroup that attends adds up the weights too
 };
 // `table` (kMaxPlanSlices entries) may be null to only size the plan.
-PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table);
+PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table);
+inline PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) { return plan_paged(d, spans ? kPagedSpans : kPagedDense, table); }
 
 // Parts of the workspace of a one-token call, in bytes from its start.
 struct PagedWorkspace {
   size_t ml, acc, final_ml, counts, list, scores, total;  // counters lie at 0
   bool sliced, weights, spans;
 };
-PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights);
+PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, PagedKind kind, bool weights);
+inline PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, bool spans, bool weights) {
+  return paged_workspace(d, p, spans ? kPagedSpans : kPagedDense, weights);
+}
 
 // How a prompt call is cut: query rows in tiles, and a tile's positions among several workgroups where there are few tiles.
 constexpr int kPromptTileRows = 128;
@@ -54,6 +61,19 @@ struct PromptPlan {
 };
 PromptPlan plan_prompt(const span_paged_desc_t* d);
 size_t prompt_workspace(const span_paged_desc_t* d, const PromptPlan& p);
+
+// Whether new rows can be turned as `r` (null: not turned) says.
+int check_rotation(const span_paged_desc_t* d, const paged_rotation_t* r);
+
+// A page of 4-bit values holds its rows' codes, then their exponents.  Both lie in groups of 16 rows, K's codes by blocks of 32 channels and in each by rows, V's by fours of rows, in
+// each by sixteenths of the channels and in those by rows, the exponents by blocks and in each by rows: what a lane of the attention kernel takes is contiguous.
+constexpr int kFp4Rows = 16, kFp4Block = 32;  // rows of a group, channels that share an exponent
+constexpr int kFp4LeastExponent = -126, kFp4MostExponent = 125;
+inline int64_t fp4_page_bytes(const span_paged_desc_t* d) { return (int64_t)d->page_size * (d->head_dim / 2 + d->head_dim / kFp4Block); }
+
+// A selection's scores, one of each page of a (sequence, KV head), behind the counters.
+int check_select(const span_paged_desc_t* d);
+size_t select_workspace(const span_paged_desc_t* d);
 
 // An eviction of longer caches keeps lists in the workspace and moves their rows in a second launch.
 constexpr int32_t kMostKeysHeld = 32768;

@@ -246,6 +246,7 @@ struct F16 : HalfQuery {
       f[2 * i + 1] = (float)h.y;
     }
   }
+  static __device__ __forceinline__ uint32_t pack2(float f0, float f1) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)f0, (_Float16)f1}); }
   static __device__ __forceinline__ uint32_t scale_query(uint32_t q, float scale) { return scaled<0x7c00u>(q, scale); }
   static __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7c00u) == 0x7c00u || (w & 0x7c000000u) == 0x7c000000u; }
   static __device__ __forceinline__ void unpack4(u32x2 r, float* f) {
@@ -294,6 +295,7 @@ struct BF16 : HalfQuery {
       f[2 * i + 1] = __builtin_bit_cast(float, w & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ uint32_t pack2(float f0, float f1) { return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f0, (__bf16)f1}); }
   static __device__ __forceinline__ uint32_t scale_query(uint32_t q, float scale) { return scaled<0x7f80u>(q, scale); }
   static __device__ __forceinline__ bool not_finite(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
   static __device__ __forceinline__ void unpack4(u32x2 r, float* f) {
