@@ -13,6 +13,7 @@ struct PagedArgs : LaunchArgs {  // heads: KV heads; max_len: positions of a seq
   int32_t batch, window, sinks;
   int32_t room, more_room;   // > 0: slices per head aimed at, see locate_slice; 0: num_splits each, or the table
   int32_t whole;             // up to so many positions a sequence is not cut
+  int32_t least;             // positions of a slice at least
   float* scores;             // [batch, kv head, query head of the group, max_len] unscaled scores by virtual position, or null
   float* final_ml;           // [batch, query head] (maximum, sum)
   int32_t* counts;           // span form with weights: [batch] attended positions
@@ -48,7 +49,7 @@ struct Slice {
 };
 
 // Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than `whole`, T whole steps and
-// kPagedLeastSlice at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
+// PagedArgs::least at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
 // many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice well above the
 // mean, which is what the whole call waits for then, `more_room` is tried.  Every workgroup works it out for itself: one load of the lengths,
 // which it needs anyway, and a few scans for up to 64 sequences.
@@ -79,7 +80,7 @@ __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lan
       T = longest;
       if (room > batch) {
         const float mean = (float)all / ((float)room - 0.5f * (float)batch);  // (a sequence has half a slice more than its share on average)
-        T = max(steps((uint32_t)mean), (uint32_t)kPagedLeastSlice);
+        T = max(steps((uint32_t)mean), (uint32_t)a.least);
         while (T < longest) {
           uint32_t total = 0;
           for (int c = 0; c < a.batch; c += 64) {
@@ -90,7 +91,7 @@ __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lan
           T = min(max(steps((uint32_t)((float)T * (float)total / (float)room)), steps(T + T / 16)), longest);
         }
       }
-      if ((float)min(T, longest) * (float)max(room, batch) <= 1.4f * (float)all || T <= (uint32_t)kPagedLeastSlice) break;
+      if ((float)min(T, longest) * (float)max(room, batch) <= 1.4f * (float)all || T <= (uint32_t)a.least) break;
     }
   }
   Slice s = {-1, 0, 1, 0, 0};
@@ -125,21 +126,20 @@ __device__ __forceinline__ void priority(int done, int quarter) {
 }
 
 // The waves' states are merged in LDS; a slice that is its sequence's only one goes out as it is, others by way of the workspace: the workgroup that arrives last
-// for the pair merges them all.  A lane holds of query column qi the reference, the sum over the wave and, in O[e][r], the unnormalised outputs of column NE (4 c4 + r) + e
-// (kSplitPieces: 64 u + 4 (4 c4 + r) + e % 4, u = e / 4); both sums are weight_scale times the weights'.  kFinal: (maximum, sum) go to final_ml.  True for the only slice.
-template <int D, int NE, bool kSplitPieces, bool kFinal>
-__device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl, int h, float ref, float lsum, const f32x4 (&O)[NE], float post, float weight_scale,
-                                            f32x2 (&s_ml)[16][kWavesPerBlock], float (&acc)[kWavesPerBlock][16][D + 4], uint32_t& s_ticket) {
-  const int tid = threadIdx.x, lane = tid & 63;
+// for the pair merges them all.  s_ml[j][wave] holds query column j's reference and the sum over the wave; put(acc[wave]) stores the wave's unnormalised outputs, [column][channel], once
+// the tables that acc lies over are no longer read; both sums are weight_scale times the weights'.  kFinal: (maximum, sum) go to final_ml.  True for the only slice.
+// kTeams: where a group has 16 / kTeams heads at most, so many teams of threads share a pair's slices out (25 slices of four heads: 3 us less, three trips to memory of eight slices each).
+template <int D, bool kFinal, int kTeams, class Put>
+__device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl, int h, float post, float weight_scale, f32x2 (&s_ml)[16][kWavesPerBlock],
+                                            float (&acc)[kWavesPerBlock][16][D + 4], uint32_t& s_ticket, Put&& put) {
+  const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int qi = lane & 15, c4 = lane >> 4;
   const int kv_heads = a.heads, group = a.group, split = sl.split, nsl = sl.nsl;
   const size_t bh = (size_t)sl.b * kv_heads + h;
   auto qrow = [&](int j) { return bh * (size_t)group + (size_t)min(j, group - 1); };
-  auto column = [&](int i, int u) { return kSplitPieces ? 64 * u + 4 * i : NE * i + 4 * u; };
-  if (c4 == 0) s_ml[qi][wave] = f32x2{ref, lsum};
   constexpr int kPerToken = kThreads / 16, kQuads = D / 4 / kPerToken;
-  const int mine = tid / kPerToken, part = tid % kPerToken;  // query head, share of its quads of columns
+  const int mine = tid % (kThreads / kTeams) / kPerToken, part = tid % kPerToken;  // query head, share of its quads of columns
+  const int team = kTeams == 1 ? 0 : wave / (kWavesPerBlock / kTeams);
   const bool direct = nsl == 1;
   const size_t slot0 = (size_t)sl.y0 * kv_heads + h, my_slot = slot0 + (size_t)split * kv_heads;
   auto acc_slot = [&](size_t slot) { return slab_resource(a.part_acc + slot * (size_t)(group * D), (uint32_t)(group * D) * 4u); };
@@ -152,41 +152,41 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
     if (kFinal && part == 0) *reinterpret_cast<f32x2*>(a.final_ml + 2 * qrow(mine)) = f32x2{M, L / weight_scale};
   };
   __syncthreads();  // the (maximum, sum) pairs are in LDS; the streaming tables are no longer read
-  if (qi < group) {
+  put(acc[wave]);
+  float M, L;
+  f32x4 o[kQuads];
+  auto join = [&](auto states) {  // of the first so many waves', or teams', states in LDS
+    constexpr int kStates = decltype(states)::value;
+    float weight[kStates];
+    f32x2 ml[kStates];
+    M = -INFINITY;
+    L = 0.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int w = 0; w < kStates; ++w) ml[w] = s_ml[mine][w];
 #pragma unroll
-      for (int u = 0; u < NE / 4; ++u)
-        *reinterpret_cast<f32x4*>(&acc[wave][qi][column(4 * c4 + r, u)]) = f32x4{O[4 * u][r], O[4 * u + 1][r], O[4 * u + 2][r], O[4 * u + 3][r]};
-    }
-  }
-  float weight[kWavesPerBlock], M = -INFINITY, L = 0.f;
-  {
-    f32x2 ml[kWavesPerBlock];
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w) ml[w] = s_ml[mine][w];
-#pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w)
+    for (int w = 0; w < kStates; ++w)
       if (ml[w][1] != 0.f) M = fmaxf(M, ml[w][0]);  // (a NaN sum counts: it has to reach the output)
 #pragma unroll
-    for (int w = 0; w < kWavesPerBlock; ++w) {
+    for (int w = 0; w < kStates; ++w) {
       weight[w] = ml[w][1] != 0.f ? __builtin_amdgcn_exp2f((ml[w][0] - M) * post) : 0.f;
       L = fmaf(weight[w], ml[w][1], L);
     }
-  }
-  __syncthreads();
-  if (mine < group) {
-    f32x4 o[kQuads];
+    __syncthreads();
+    if (mine < group && team == 0) {
 #pragma unroll
-    for (int i = 0; i < kQuads; ++i) {
-      o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < kQuads; ++i) {
+        o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWavesPerBlock; ++w) {
-        const f32x4 ow = *reinterpret_cast<const f32x4*>(&acc[w][mine][4 * (part + kPerToken * i)]);
+        for (int w = 0; w < kStates; ++w) {
+          const f32x4 ow = *reinterpret_cast<const f32x4*>(&acc[w][mine][4 * (part + kPerToken * i)]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[i][k] = fmaf(weight[w], ow[k], o[i][k]);
+          for (int k = 0; k < 4; ++k) o[i][k] = fmaf(weight[w], ow[k], o[i][k]);
+        }
       }
     }
+  };
+  join(std::integral_constant<int, kWavesPerBlock>());
+  if (mine < group && team == 0) {
     if (direct) {
       store_row(M, L, o);
     } else {
@@ -206,17 +206,16 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
   if (s_ticket != (uint32_t)(nsl - 1)) return false;
   if (mine < group) {
     constexpr int kMerge = 8;
-    f32x4 o[kQuads];
 #pragma unroll
     for (int i = 0; i < kQuads; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     M = -INFINITY;
     L = 0.f;
-    for (int s0 = 0; s0 < nsl; s0 += kMerge) {
+    for (int s0 = team; s0 < nsl; s0 += kTeams * kMerge) {
       f32x2 ml[kMerge];
       f32x4 os[kMerge][kQuads];
 #pragma unroll
       for (int k = 0; k < kMerge; ++k) {
-        const size_t slot = slot0 + (size_t)min(s0 + k, nsl - 1) * kv_heads;  // (past the end: a slot that exists, unused)
+        const size_t slot = slot0 + (size_t)min(s0 + kTeams * k, nsl - 1) * kv_heads;  // (past the end: a slot that exists, unused)
         ml[k] = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(ml_slot(slot), (uint32_t)mine * 8u, 0, kThrough));
         const __amdgpu_buffer_rsrc_t states = acc_slot(slot);
 #pragma unroll
@@ -225,11 +224,11 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
       const float before = M;
 #pragma unroll
       for (int k = 0; k < kMerge; ++k) {
-        if (s0 + k >= nsl) ml[k][1] = 0.f;
+        if (s0 + kTeams * k >= nsl) ml[k][1] = 0.f;
         if (ml[k][1] != 0.f) M = fmaxf(M, ml[k][0]);
       }
       const float safe = M == -INFINITY ? 0.f : M;
-      if (s0 > 0) {
+      if (s0 > team) {
         const float old = __builtin_amdgcn_exp2f((before - safe) * post);
         L *= old;
 #pragma unroll
@@ -237,7 +236,7 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
       }
 #pragma unroll
       for (int k = 0; k < kMerge; ++k) {
-        if (s0 + k < nsl) {
+        if (s0 + kTeams * k < nsl) {
           const float w = ml[k][1] != 0.f ? __builtin_amdgcn_exp2f((ml[k][0] - safe) * post) : 0.f;
           L = fmaf(w, ml[k][1], L);
 #pragma unroll
@@ -248,7 +247,18 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
         }
       }
     }
-    store_row(M, L, o);
+    if constexpr (kTeams == 1) {
+      store_row(M, L, o);
+    } else {
+      if (part == 0) s_ml[mine][team] = f32x2{M, L};
+#pragma unroll
+      for (int i = 0; i < kQuads; ++i) *reinterpret_cast<f32x4*>(&acc[team][mine][4 * (part + kPerToken * i)]) = o[i];
+    }
+  }
+  if constexpr (kTeams > 1) {
+    __syncthreads();
+    join(std::integral_constant<int, kTeams>());
+    if (mine < group && team == 0) store_row(M, L, o);
   }
   if (tid == 0) __hip_atomic_store(a.counters + bh * (size_t)a.counter_stride, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return false;
@@ -257,7 +267,7 @@ __device__ __forceinline__ bool finish_pair(const PagedArgs& a, const Slice& sl,
 // Arguments and plan of a one-token call, or what it is refused with.  `table`: kMaxPlanSlices entries.
 inline int one_token_args(const span_paged_desc_t* d, PagedKind kind, const void* q, const void* k, const void* v, const int32_t* block_table,
                           const int32_t* ctx_lens, const int32_t* offsets, const int32_t* starts, const int32_t* ends, const int32_t* selected, float scale,
-                          float* weights, float* out, PagedArgs* args, PagedPlan* plan, uint32_t* table) {
+                          float* weights, float* out, PagedArgs* args, PagedPlan* plan, uint32_t* table, bool fp4 = false) {
   const bool spans = kind == kPagedSpans;
   const int rc = check_paged(d);
   if (rc != SPAN_OK) return rc;
@@ -265,7 +275,7 @@ inline int one_token_args(const span_paged_desc_t* d, PagedKind kind, const void
   if (spans ? !offsets || (d->num_intervals > 0 && (!starts || !ends)) : !ctx_lens) return SPAN_ERR_NULL;
   if (kind == kPagedSelected && (d->budget < 1 || !selected)) return d->budget < 1 ? SPAN_ERR_SHAPE : SPAN_ERR_NULL;
   const PagedPlan& p = *plan;
-  *plan = plan_paged(d, kind, table);
+  *plan = plan_paged(d, kind, table, fp4);
   const PagedWorkspace w = paged_workspace(d, p, kind, weights != nullptr);
   if (w.total > 0 && (!d->workspace || ((uintptr_t)d->workspace & 255u) || d->workspace_bytes < w.total)) return SPAN_ERR_WORKSPACE;
   char* at = (char*)d->workspace;
@@ -298,7 +308,8 @@ inline int one_token_args(const span_paged_desc_t* d, PagedKind kind, const void
   a.sinks = d->sinks;
   a.room = p.cut ? p.room : 0;
   a.more_room = p.rows;
-  a.whole = paged_whole(d);
+  a.whole = paged_whole(d, fp4);
+  a.least = paged_least(fp4);
   a.final_ml = weights ? (float*)(at + w.final_ml) : nullptr;
   a.counts = weights && spans ? (int32_t*)(at + w.counts) : nullptr;
   a.list = weights && spans ? (int32_t*)(at + w.list) : nullptr;

@@ -460,7 +460,17 @@ __attribute__((amdgpu_waves_per_eu(PagedShape<Elt, D>::kWaves, PagedShape<Elt, D
 
   // ---- the waves' states, and the slices', are merged --------------------------------------------------
   lsum = across_groups_sum<16>(lsum) * Elt::kWeightScale;
-  const bool whole = finish_pair<D, NE, kSplitPieces, kWeights>(a, sl, h, ref, lsum, O, post, Elt::kWeightScale, s_ml, s_u.ws.acc, s_ticket);
+  if (c4 == 0) s_ml[qi][wave] = f32x2{ref, lsum};
+  const bool whole = finish_pair<D, kWeights, 1>(a, sl, h, post, Elt::kWeightScale, s_ml, s_u.ws.acc, s_ticket, [&](float (&acc)[16][kAccRow]) {
+    if (qi < group) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int u = 0; u < NE / 4; ++u)
+          *reinterpret_cast<f32x4*>(&acc[qi][column(4 * c4 + r, u)]) = f32x4{O[4 * u][r], O[4 * u + 1][r], O[4 * u + 2][r], O[4 * u + 3][r]};
+      }
+    }
+  });
   if (kWeights && whole && a.weights_here) {  // (no sequence of the call is cut: nothing else is waited for)
     __syncthreads();                          // scores, list and final states are written
     for (int v0 = 4 * tid; v0 < n_total; v0 += 4 * kThreads) add_weights<Elt, kSpans>(a, seen, n_total, b, h, v0);

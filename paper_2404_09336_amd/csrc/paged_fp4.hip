@@ -6,8 +6,12 @@
 //     time, and every load is contiguous over the wave.  Where a window, a span or the cache begins or ends inside a unit, its other rows are masked; two intervals that meet in a unit are two units.
 //   * K stays as it is: fp4 x fp6 products with both exponents applied by the matrix core.  q is laid out as kDigits digits to the base 16, each -16 .. 16 times a power of two that 32 channels share:
 //     such a digit is an fp6 value (E2M3) exactly.  (The matrix core adds eight neighbouring products up with some 13 bits below the largest, measured; products of digits fit that, those of
-//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block, six 25.
-//   * V becomes bf16, exactly, times its exponent: one instruction for two values, and one for each two that brings neighbouring positions together.  Weights meet it in three bf16 terms, all 24 bits.
+//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block.
+//   * V becomes bf16, exactly, times its exponent: one instruction for two channels.  Weights meet it as two bf16 terms, each rounded, which together hold 17 bits at least (off by 2^-18 of the weight; a
+//     third would cost a quarter of the step's instructions, for a cache whose values are rounded to two bits).
+//   * A step of 32 positions is bound by the instructions that a SIMD issues, not by the matrix core, and few heads leave columns free.  With up to 8 heads a head has two columns,
+//     for even and odd channels: its weights go to every other of the product's inner places, zeros between them, and two channels of a row, as the conversion leaves them, need not be parted.  With up to 4
+//     heads it has four, and the two terms go through one product.
 #include "paged_attend.h"
 
 namespace spanattn {
@@ -15,16 +19,19 @@ namespace spanattn {
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
 typedef const SPAN_GLOBAL uint8_t* global_u8;
 typedef const SPAN_GLOBAL uint32_t* global_u32;
 
 constexpr int kUnitRows = kFp4Rows;
 constexpr int kStepUnits = 2;                  // units that a wave takes together: 32 positions of one product with V
 constexpr int kStepRows = kUnitRows * kStepUnits;
+// The reference of the weights is moved on when a score's weight would pass 2^kSlack (fp32 holds those as exactly).  Whenever the maximum moves: 57 instructions more in most of a wave's first steps.
+constexpr float kSlack = 16.f;
 constexpr int kHeldUnits = 64;                 // of a wave, found at a time: one per lane
 
-template <class Elt>
-constexpr int kDigitsOf = Elt::kBytes == 4 ? 6 : 5;
+constexpr int kDigits = 5;
 
 // Units of a dense call: those of the first `sinks` positions, then those from `low` on.
 struct SeenUnits {
@@ -54,67 +61,88 @@ __device__ __forceinline__ uint32_t unit_mask(int u, int from, int to) {
   return ((1u << hi) - 1u) & ~((1u << lo) - 1u);
 }
 
+// q in LDS: of each head and block of 32 channels the fp6 codes of every digit, and the digits' exponent bytes (of digit t byte t).
+template <int D>
+struct DigitTables {
+  uint32_t codes[kDigits][16][D / 32][6];
+  uint8_t exps[16][D / 32][8];
+};
+
+// What a thread loads for its (block, digit) number i ...
 template <class Elt, int D>
-__device__ __forceinline__ void lay_digits(const PagedArgs& a, size_t row0, int group, uint32_t (*s_digits)[16][D / 32][6], uint8_t (*s_exps)[16][D / 32]) {
-  constexpr int kDigits = kDigitsOf<Elt>, kHalves = D / 16;  // sixteen channels of one digit per thread
-  for (int i = threadIdx.x; i < 16 * kHalves * kDigits; i += kThreads) {
-    const int half = i % kHalves, j = i / kHalves % 16, t = i / (kHalves * 16);
-    const int block = half / 2, word = half % 2 * 3;
-    if (j >= group) {
-      for (int w = 0; w < 3; ++w) s_digits[t][j][block][word + w] = 0u;
-      s_exps[t][j][block] = 127;
-      continue;
-    }
-    float x[16];
-    const u32x4* from = (const u32x4*)((const char*)a.q + (row0 + (size_t)j) * (size_t)(D * Elt::kBytes) + (size_t)(half * 16 * Elt::kBytes));
+struct QueryBlock {
+  u32x4 piece[2 * Elt::kBytes];
+  __device__ __forceinline__ void load(const PagedArgs& a, size_t row0, int i) {
+    const int block = i % (D / 32), j = i / (D / 32 * kDigits);
+    const u32x4* from = (const u32x4*)((const char*)a.q + (row0 + (size_t)j) * (size_t)(D * Elt::kBytes) + (size_t)(block * 32 * Elt::kBytes));
 #pragma unroll
-    for (int p = 0; p < Elt::kBytes; ++p) {
-      u32x4 piece = from[p];
+    for (int p = 0; p < 2 * Elt::kBytes; ++p) piece[p] = from[p];
+  }
+  // ... and the digit's codes.
+  __device__ __forceinline__ void lay(const PagedArgs& a, int i, DigitTables<D>& tab) {
+    const int block = i % (D / 32), t = i / (D / 32) % kDigits, j = i / (D / 32 * kDigits);
+    float x[32];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) piece[k] = Elt::scale_query(piece[k], a.scale_log2e);
-      Elt::unpack(piece, x + p * Elt::kPerVec);
+    for (int p = 0; p < 2 * Elt::kBytes; ++p) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) piece[p][k] = Elt::scale_query(piece[p][k], a.scale_log2e);
+      Elt::unpack(piece[p], x + p * Elt::kPerVec);
     }
     uint32_t most = 0;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) most = max(most, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
-    most = max(most, (uint32_t)dpp_i<0xB1>((int)most));  // the block's other half is the next thread's
+    for (int k = 0; k < 32; ++k) most = max(most, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
     // |x| < 2^(e - 126), e the largest's exponent bits; digit t counts 2^(e - 126 - 4 (t + 1)), as an fp6 value 8 times that each
     const int e = max((int)(most >> 23), 1);
     const int scale = e - 126 - 4 * (t + 1) + 3 + 127;
-    s_exps[t][j][block] = (uint8_t)(most >= 0x7f800000u ? 255 : max(scale, 0));  // (not finite: NaN)
-    uint32_t words[3] = {0u, 0u, 0u};
+    tab.exps[j][block][t] = (uint8_t)(most >= 0x7f800000u ? 255 : max(scale, 0));  // (not finite: NaN)
+    // What the digits ahead of this one leave, x less its nearest multiple of the last one's unit, is the digit times 2^-4 when rounded to a whole number of them: that is how
+    // fp6 values up to 2 are spaced.  (Ties fall the same way for all threads.  The conversion takes its values from the two vectors in turn.)
+    f32x16 half[2];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      // what the digits ahead of this one leave: x less its nearest multiple of the last one's unit (ties fall the same way for all threads)
-      const float y = ldexpf(x[k], 126 - e + 4 * t), rest = t == 0 ? y : y - rintf(y);
-      const int digit = (int)rintf(rest * 16.f);
-      const uint32_t code = scale < 0 ? 0u : (uint32_t)abs(digit) | (digit < 0 ? 32u : 0u);
-      const int bit = 6 * k;
-      words[bit / 32] |= code << (bit % 32);
-      if (bit % 32 > 26) words[bit / 32 + 1] |= code >> (32 - bit % 32);
+    for (int k = 0; k < 32; ++k) {
+      const float y = __builtin_amdgcn_ldexpf(x[k], 126 - e + 4 * t);
+      half[k % 2][k / 2] = scale < 0 ? 0.f : y - (t == 0 ? 0.f : rintf(y));
     }
-    for (int w = 0; w < 3; ++w) s_digits[t][j][block][word + w] = words[w];
+    const u32x6 codes = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(half[0], half[1], 0.5f);
+#pragma unroll
+    for (int w = 0; w < 6; ++w) tab.codes[t][j][block][w] = codes[w];
+  }
+};
+
+// sums += K (16 rows, fp4) x digit t of q (16 heads, fp6), both with their exponents.
+__device__ __forceinline__ f32x4 digit_product(i32x8 k, int k_exp, i32x8 q, u32x2 q_exps, int t, f32x4 sums) {
+  const int low = (int)q_exps[0], high = (int)q_exps[1];
+  switch (t) {  // (which byte of the exponents is part of the instruction)
+    case 0:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 0, low);
+    case 1:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 1, low);
+    case 2:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 2, low);
+    case 3:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 3, low);
+    default:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 0, high);
   }
 }
 
-template <class Elt, int D, PagedKind kKind, class Args>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))) void fp4_kernel(const Args a) {
+// kShare: columns that a query head has, 1, 2 or 4.
+template <class Elt, int D, PagedKind kKind, int kShare, class Args>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))) void fp4_kernel(const Args a) {
   constexpr bool kSpans = kKind == kPagedSpans;
-  constexpr int kDigits = kDigitsOf<Elt>, kBlocks = D / 32, NE = D / 16;
+  constexpr int NE = D / 16;              // V channels of a lane
+  constexpr int kHeads = 16 / kShare;     // heads that the columns hold
+  constexpr int kSums = kShare == 1 ? NE : NE / 2;
   constexpr uint32_t kUnitBytes = 8u * D, kUnitExps = D / 2u;
-  constexpr int kAccRow = D + 4, kTerms = 3;
+  constexpr int kAccRow = D + 4;
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qi = lane & 15, c4 = lane >> 4;
   const int h = blockIdx.x, kv_heads = a.heads, group = a.group;
 
-  struct Queries {
-    uint32_t digits[kDigits][16][kBlocks][6];
-    uint8_t exps[kDigits][16][kBlocks];
-  };
   union Overlaid {
-    Queries q;
+    DigitTables<D> q;
     float acc[kWavesPerBlock][16][kAccRow];
   };
   __shared__ __attribute__((aligned(16))) Overlaid s_u;
@@ -140,7 +168,9 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
   const int32_t* table = a.block_table + (size_t)b * a.table_pages;
   const float post = Elt::post_scale(a.scale_log2e);  // weight = exp2((score - largest score) * post)
 
-  lay_digits<Elt, D>(a, bh * (size_t)group, group, s_u.q.digits, s_u.q.exps);
+  const int q_parts = group * (D / 32) * kDigits;  // (block, digit) pairs, a thread's at a time
+  QueryBlock<Elt, D> q_block0;
+  if (tid < q_parts) q_block0.load(a, bh * (size_t)group, tid);
 
   SeenUnits seen = {0, 0, 0, 0};
   int first_interval = 0, intervals = 0, all;  // units of the sequence
@@ -174,7 +204,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
   const uint32_t exps_at = (uint32_t)(D / 2) << a.page_shift;
 
   // The wave's units from its unit w0 on, one per lane: unit of the pool (page * units of a page + unit in the page) and mask of the rows that take part.
-  int held_unit = 0;
+  int held_unit = 0, held_at = 0;
   uint32_t held_mask = 0;
   auto find_units = [&](int w0) {
     const int w = w0 + lane, s = step0 + wave + w / kStepUnits * kWavesPerBlock;
@@ -207,121 +237,132 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
       u = sink ? v : v - seen.first + seen.low / kUnitRows;
       if (mine) held_mask = unit_mask(u, sink ? 0 : seen.low, sink ? seen.sinks : seen.held);
     }
-    int x = -1;
-    if (mine && held_mask != 0) x = pool_row(table, u * kUnitRows, a.page_shift, a.num_pages);
-    if (x < 0) held_mask = 0;
-    held_unit = max(x, 0) / kUnitRows;  // (none: the pool's first, which nobody attends)
+    held_unit = -1;
+    if (mine && held_mask != 0) {
+      held_unit = table[u >> unit_shift];  // the page, until take_units
+      held_at = u & ((1 << unit_shift) - 1);
+    }
+  };
+  auto take_units = [&]() {
+    const bool there = (uint32_t)held_unit < (uint32_t)a.num_pages;
+    if (!there) held_mask = 0;
+    held_unit = there ? (held_unit << unit_shift) + held_at : 0;  // (none: the pool's first, which nobody attends)
   };
 
   float ref = -INFINITY, lsum = 0.f;
-  f32x4 O[NE];
+  // Unnormalised outputs.  kShare 1: O[e][r] of column qi's head, channel NE (4 c4 + r) + e.  Otherwise O[p][r], channel NE (4 c4 + r) + 2 p + odd; kShare 4: the term's part of it.
+  f32x4 O[kSums];
 #pragma unroll
-  for (int e = 0; e < NE; ++e) O[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int e = 0; e < kSums; ++e) O[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const int role = qi / kHeads;                    // of the column among its head's
+  const bool odd = kShare > 1 && (role & 1);       // the channels that it sums
+  const bool second = kShare == 4 && role >= 2;    // the term that it brings
+  // Selectors of byte permutations: a bf16 value (of two in a dword, by the row's parity) as fp32 for lanes that take the first term away, 0 for the others; its place in the product's operand.
+  const uint32_t sel_first[2] = {kShare == 4 && !second ? 0x0c0c0c0cu : 0x01000c0cu, kShare == 4 && !second ? 0x0c0c0c0cu : 0x03020c0cu};
+  const uint32_t sel_place[2] = {odd ? 0x01000c0cu : 0x0c0c0100u, odd ? 0x03020c0cu : 0x0c0c0302u};
 
   // What a lane holds of a unit.  D = 128: K of row qi, channels 32 c4 on; D = 64: of two units together, K of row qi, unit c4 / 2, channels 32 (c4 % 2) on.  V of rows 4 c4 .. + 3, channels NE qi on.
+  // A step's loads are under way while the step before it is worked on.
   constexpr int kKLoads = D == 128 ? kStepUnits : kStepUnits / 2;
-  u32x4 kr[kKLoads];
-  uint32_t ke[kKLoads];
-  uint32_t vr[kStepUnits][4 * NE / 8];  // D = 128: a dword a row; 64: half of one
-  uint32_t ve[kStepUnits];              // exponents of its four rows
-  uint32_t mask[kStepUnits];
-  const char *ku[kStepUnits], *vu[kStepUnits];  // (scalar)
-  uint32_t eu[kStepUnits];
-  auto locate = [&](int w) {  // units w, w + 1 of those held
+  u32x4 kr[2][kKLoads];
+  uint32_t ke[2][kKLoads];
+  uint32_t vr[2][kStepUnits][4 * NE / 8];  // D = 128: a dword a row; 64: half of one
+  uint32_t ve[2][kStepUnits];              // exponents of its four rows
+  uint32_t mask[2][kStepUnits];
+  auto fetch = [&](int w, auto place) {  // units w, w + 1 of those held
+    constexpr int kTo = decltype(place)::value;
+    const char SPAN_GLOBAL *ku[kStepUnits], *vu[kStepUnits];  // (scalar)
+    uint32_t eu[kStepUnits];                                  // from a unit's codes to its exponents
+    int ln = lane;
+    asm volatile("" : "+v"(ln));  // (offsets are worked out here, next to the scalar addresses, and not kept)
+    const uint32_t l = (uint32_t)ln;
+    const uint32_t v_exp_off = 16u * ((l & 15u) * NE / kFp4Block) + 4u * (l >> 4);
 #pragma unroll
     for (int i = 0; i < kStepUnits; ++i) {
       const uint32_t x = (uint32_t)__builtin_amdgcn_readlane(held_unit, w + i);
-      mask[i] = (uint32_t)__builtin_amdgcn_readlane((int)held_mask, w + i);
+      mask[kTo][i] = (uint32_t)__builtin_amdgcn_readlane((int)held_mask, w + i);
       const uint32_t page = x >> unit_shift, in_page = x & ((1u << unit_shift) - 1u);
-      const size_t at = (size_t)page * page_stride;
-      ku[i] = k_head + at + in_page * kUnitBytes;
-      vu[i] = v_head + at + in_page * kUnitBytes;
-      eu[i] = exps_at - in_page * (kUnitBytes - kUnitExps);  // from a unit's codes to its exponents
+      const size_t at = (size_t)page * page_stride + in_page * kUnitBytes;
+      ku[i] = (const char SPAN_GLOBAL*)(uintptr_t)(k_head + at);
+      vu[i] = (const char SPAN_GLOBAL*)(uintptr_t)(v_head + at);
+      eu[i] = exps_at - in_page * (kUnitBytes - kUnitExps);
     }
-  };
-  auto load_k = [&]() {
     if constexpr (D == 128) {
 #pragma unroll
       for (int i = 0; i < kStepUnits; ++i) {
-        kr[i] = __builtin_nontemporal_load((global_u32x4)(uintptr_t)(ku[i] + 16u * (uint32_t)lane));
-        ke[i] = *(global_u8)(uintptr_t)(ku[i] + eu[i] + (uint32_t)lane);
+        kr[kTo][i] = __builtin_nontemporal_load((global_u32x4)(ku[i] + 16u * l));
+        ke[kTo][i] = *(global_u8)(ku[i] + eu[i] + l);
       }
     } else {
-      const char* at = lane < 32 ? ku[0] : ku[1];
-      const uint32_t l = (uint32_t)lane & 31u;
-      kr[0] = __builtin_nontemporal_load((global_u32x4)(uintptr_t)(at + 16u * l));
-      ke[0] = *(global_u8)(uintptr_t)(at + (lane < 32 ? eu[0] : eu[1]) + l);
+      const char SPAN_GLOBAL* at = l < 32 ? ku[0] : ku[1];
+      kr[kTo][0] = __builtin_nontemporal_load((global_u32x4)(at + 16u * (l & 31u)));
+      ke[kTo][0] = *(global_u8)(at + (l < 32 ? eu[0] : eu[1]) + (l & 31u));
     }
-  };
-  auto load_v = [&]() {
 #pragma unroll
     for (int i = 0; i < kStepUnits; ++i) {
       if constexpr (D == 128) {
-        const u32x4 w = __builtin_nontemporal_load((global_u32x4)(uintptr_t)(vu[i] + 16u * (uint32_t)lane));
+        const u32x4 x = __builtin_nontemporal_load((global_u32x4)(vu[i] + 16u * l));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) vr[i][k] = w[k];
+        for (int k = 0; k < 4; ++k) vr[kTo][i][k] = x[k];
       } else {
-        const u32x2 w = __builtin_nontemporal_load((global_u32x2)(uintptr_t)(vu[i] + 8u * (uint32_t)lane));
-        vr[i][0] = w[0];
-        vr[i][1] = w[1];
+        const u32x2 x = __builtin_nontemporal_load((global_u32x2)(vu[i] + 8u * l));
+        vr[kTo][i][0] = x[0];
+        vr[kTo][i][1] = x[1];
       }
-      ve[i] = *(global_u32)(uintptr_t)(vu[i] + eu[i] + 16u * (uint32_t)(qi * NE / kFp4Block) + 4u * (uint32_t)c4);
+      ve[kTo][i] = *(global_u32)(vu[i] + eu[i] + v_exp_off);
     }
   };
 
-  i32x8 q_digits[kDigits];
-  uint32_t q_exps[kDigits];
-  auto load_queries = [&]() {
-    const int block = D == 128 ? c4 : c4 & 1;
-#pragma unroll
-    for (int t = 0; t < kDigits; ++t) {
-#pragma unroll
-      for (int w = 0; w < 6; ++w) q_digits[t][w] = (int)s_u.q.digits[t][qi][block][w];
-      q_digits[t][6] = q_digits[t][7] = 0;
-      q_exps[t] = s_u.q.exps[t][qi][block];
-    }
-  };
+  const int q_row = min(qi % kHeads, group - 1), q_block = D == 128 ? c4 : c4 & 1;  // (columns past the group are its last head's, never written)
+  u32x2 q_exps = {0u, 0u};
 
-  auto step = [&](bool more, int next) {
-    // scores: sc[s][r] = column qi against row 4 c4 + r of unit s
+  auto step = [&](auto place, bool more, int next) {
+    constexpr int kAt = decltype(place)::value;
+    auto& V = vr[kAt];
+    auto& Ve = ve[kAt];
+    if (more) fetch(next, std::integral_constant<int, 1 - kAt>());
+    // scores: sc[s][r] = column qi against row 4 c4 + r of unit s.  A digit is read while the one before it is worked on, and not kept across the steps.
     f32x4 sc[kStepUnits];
 #pragma unroll
-    for (int s = 0; s < kStepUnits; ++s) {
-      i32x8 k = {0, 0, 0, 0, 0, 0, 0, 0};
-      uint32_t e = ke[D == 128 ? s : 0];
+    for (int s = 0; s < kStepUnits; ++s) sc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 digit[2];
+    auto read_digit = [&](int t, i32x8& to) {
+      asm volatile("" ::: "memory");
 #pragma unroll
-      for (int w = 0; w < 4; ++w) k[w] = (int)kr[D == 128 ? s : 0][w];
-      if constexpr (D == 64) {  // the other unit's lanes: zeros
-        const bool here = (lane < 32) == (s == 0);
+      for (int w = 0; w < 6; ++w) to[w] = (int)s_u.q.codes[t][q_row][q_block][w];
+      to[6] = to[7] = 0;
+    };
+    read_digit(kDigits - 1, digit[(kDigits - 1) & 1]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) k[w] = here ? k[w] : 0;
-        e = here ? e : 0u;
+    for (int t = kDigits - 1; t >= 0; --t) {
+      if (t > 0) read_digit(t - 1, digit[(t - 1) & 1]);
+#pragma unroll
+      for (int s = 0; s < kStepUnits; ++s) {
+        i32x8 k = {0, 0, 0, 0, 0, 0, 0, 0};
+        uint32_t e = ke[kAt][D == 128 ? s : 0];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) k[w] = (int)kr[kAt][D == 128 ? s : 0][w];
+        if constexpr (D == 64) {  // the other unit's lanes: zeros
+          const bool here = (lane < 32) == (s == 0);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) k[w] = here ? k[w] : 0;
+          e = here ? e : 0u;
+        }
+        sc[s] = digit_product(k, (int)e, digit[t & 1], q_exps, t, sc[s]);
       }
-      sc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int t = kDigits - 1; t >= 0; --t)
-        sc[s] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q_digits[t], sc[s], 4, 2, 0, (int)e, 0, (int)q_exps[t]);
     }
-    uint32_t here[kStepUnits];
     bool plain = true;
 #pragma unroll
-    for (int s = 0; s < kStepUnits; ++s) {
-      here[s] = mask[s];
-      plain = plain && here[s] == 0xffffu;
-    }
-    if (more) {
-      locate(next);
-      load_k();
-    }
+    for (int s = 0; s < kStepUnits; ++s) plain = plain && mask[kAt][s] == 0xffffu;
     if (!plain) {
 #pragma unroll
       for (int s = 0; s < kStepUnits; ++s) {
-        const uint32_t rows = here[s] >> (4 * c4) & 15u;
+        const uint32_t rows = mask[kAt][s] >> (4 * c4) & 15u;
 #pragma unroll
         for (int r = 0; r < 4; ++r) sc[s][r] = rows >> r & 1u ? sc[s][r] : -INFINITY;
         // an exponent that says NaN must not meet a weight of zero: codes of exponent 0 are finite
         const uint32_t bytes = (rows & 1u ? 0xffu : 0u) | (rows & 2u ? 0xff00u : 0u) | (rows & 4u ? 0xff0000u : 0u) | (rows & 8u ? 0xff000000u : 0u);
-        ve[s] &= bytes;
+        Ve[s] &= bytes;
       }
     }
     float mx = -INFINITY;
@@ -330,102 +371,157 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(3, 3))
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[s][r]);
     }
-    if (__builtin_amdgcn_ballot_w64(mx > ref) != 0) {
+    if (__builtin_amdgcn_ballot_w64((mx - ref) * post > kSlack) != 0) {  // (first of all: ref is -infinity)
       mx = across_groups_max<16>(mx);
       const float ref_new = fmaxf(ref, mx), ref_safe = ref_new == -INFINITY ? 0.f : ref_new;
       const float alpha = __builtin_amdgcn_exp2f((ref - ref_safe) * post);
       ref = ref_new;
       lsum *= alpha;
 #pragma unroll
-      for (int e = 0; e < NE; ++e) O[e] *= alpha;
+      for (int e = 0; e < kSums; ++e) O[e] *= alpha;
     }
     const float ref_safe = ref == -INFINITY ? 0.f : ref;
-    uint32_t terms[kTerms][2 * kStepUnits];
+    // Weights as the products' operands, the smaller terms first.  kShare 1: of all 32 rows, two in a dword; otherwise of a unit's, one in a dword.
+    constexpr int kPasses = kShare == 4 ? 1 : 2;
+    u32x4 pairs[2], terms[kPasses][kStepUnits];
 #pragma unroll
     for (int s = 0; s < kStepUnits; ++s) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) sc[s][r] = __builtin_amdgcn_exp2f((sc[s][r] - ref_safe) * post);
       lsum += (sc[s][0] + sc[s][1]) + (sc[s][2] + sc[s][3]);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint32_t tt[kTerms];
-        BF16::template split<kTerms>(sc[s][2 * k], sc[s][2 * k + 1], tt);
+      for (int k = 0; k < 2; ++k) {  // two rows
+        const uint32_t first = BF16::pack2(sc[s][2 * k], sc[s][2 * k + 1]);
+        float rest[2];
 #pragma unroll
-        for (int i = 0; i < kTerms; ++i) terms[i][2 * s + k] = tt[i];
+        for (int r = 0; r < 2; ++r) rest[r] = sc[s][2 * k + r] - __builtin_bit_cast(float, __builtin_amdgcn_perm(first, first, sel_first[r]));
+        const uint32_t last = BF16::pack2(rest[0], rest[1]);
+        if constexpr (kShare == 1) {
+          pairs[1][2 * s + k] = first;
+          pairs[0][2 * s + k] = last;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            if constexpr (kShare == 2) terms[1][s][2 * k + r] = __builtin_amdgcn_perm(first, first, sel_place[r]);
+            terms[0][s][2 * k + r] = __builtin_amdgcn_perm(last, last, sel_place[r]);
+          }
+        }
       }
     }
-    // V: two channels of a row at a time, then two rows of a channel together
+    // V: two channels of a row at a time
 #pragma unroll
     for (int p = 0; p < NE / 2; ++p) {
-      uint32_t two[kStepUnits][4];
+      u32x4 two[kStepUnits];
 #pragma unroll
       for (int s = 0; s < kStepUnits; ++s) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           // (the conversion takes the exponent bits alone: what lies around them does not matter)
-          const float scale = __builtin_bit_cast(float, r < 3 ? ve[s] << (23 - 8 * r) : ve[s] >> 1);
-          if constexpr (D == 128) {
-            two[s][r] = p == 0   ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vr[s][r], scale, 0))
-                        : p == 1 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vr[s][r], scale, 1))
-                        : p == 2 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vr[s][r], scale, 2))
-                                 : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vr[s][r], scale, 3));
-          } else {
-            const uint32_t w = vr[s][r / 2];  // two rows of four channels
-            const int byte = 2 * (r % 2) + p;
-            two[s][r] = byte == 0   ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0))
-                        : byte == 1 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1))
-                        : byte == 2 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2))
-                                    : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
-          }
+          const float scale = __builtin_bit_cast(float, r < 3 ? Ve[s] << (23 - 8 * r) : Ve[s] >> 1);
+          const uint32_t w = D == 128 ? V[s][r] : V[s][r / 2];  // (64: two rows of four channels)
+          const int byte = D == 128 ? p : 2 * (r % 2) + p;
+          const bf16x2 v = byte == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+                           : byte == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+                           : byte == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                                       : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+          two[s][r] = __builtin_bit_cast(uint32_t, v);
         }
       }
+      if constexpr (kShare == 1) {  // the two rows of a channel together
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t sel = k ? 0x07060302u : 0x05040100u;
-        const u32x4 v = {__builtin_amdgcn_perm(two[0][1], two[0][0], sel), __builtin_amdgcn_perm(two[0][3], two[0][2], sel),
-                         __builtin_amdgcn_perm(two[1][1], two[1][0], sel), __builtin_amdgcn_perm(two[1][3], two[1][2], sel)};
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t sel = k ? 0x07060302u : 0x05040100u;
+          const u32x4 v = {__builtin_amdgcn_perm(two[0][1], two[0][0], sel), __builtin_amdgcn_perm(two[0][3], two[0][2], sel),
+                           __builtin_amdgcn_perm(two[1][1], two[1][0], sel), __builtin_amdgcn_perm(two[1][3], two[1][2], sel)};
 #pragma unroll
-        for (int i = kTerms - 1; i >= 0; --i) O[2 * p + k] = BF16::mfma(v, u32x4{terms[i][0], terms[i][1], terms[i][2], terms[i][3]}, O[2 * p + k]);
+          for (int i = 0; i < 2; ++i) O[2 * p + k] = BF16::mfma(v, pairs[i], O[2 * p + k]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) {
+#pragma unroll
+          for (int s = 0; s < kStepUnits; ++s) O[p] = BF16::mfma(two[s], terms[i][s], O[p]);
+        }
       }
     }
-    if (more) load_v();
   };
 
+  if (steps > 0) find_units(0);
+  if (tid < q_parts) q_block0.lay(a, tid, s_u.q);  // (while the table's entries are on their way)
   if (steps > 0) {
-    find_units(0);
-    locate(0);
-    load_k();
-    load_v();
+    take_units();
+    fetch(0, std::integral_constant<int, 0>());
   }
-  __syncthreads();  // q's digits are laid out
-  load_queries();
-  for (int w = 0; w < steps * kStepUnits; w += kStepUnits) {
+  for (int i = tid + kThreads; i < q_parts; i += kThreads) {
+    QueryBlock<Elt, D> more;
+    more.load(a, bh * (size_t)group, i);
+    more.lay(a, i, s_u.q);
+  }
+  __syncthreads();
+  q_exps = *reinterpret_cast<const u32x2*>(s_u.q.exps[q_row][q_block]);
+  const int units = steps * kStepUnits;
+  auto next_of = [&](int w) {
     const int next = w + kStepUnits;
-    const bool more = next < steps * kStepUnits;
-    if (more && next % kHeldUnits == 0) find_units(next);
-    step(more, next % kHeldUnits);
+    if (next < units && next % kHeldUnits == 0) {
+      find_units(next);
+      take_units();
+    }
+    return next;
+  };
+  for (int w = 0; w < units; w += 2 * kStepUnits) {
+    int next = next_of(w);
+    step(std::integral_constant<int, 0>(), next < units, next % kHeldUnits);
+    if (next >= units) break;
+    next = next_of(next);
+    step(std::integral_constant<int, 1>(), next < units, next % kHeldUnits);
   }
   lsum = across_groups_sum<16>(lsum);
   __syncthreads();  // q's digits are read by all: the states go where they were
-  finish_pair<D, NE, false, false>(a, sl, h, ref, lsum, O, post, 1.f, s_ml, s_u.acc, s_ticket);
+  if (c4 == 0 && qi < kHeads) s_ml[qi][wave] = f32x2{ref, lsum};
+  finish_pair<D, false, kShare>(a, sl, h, post, 1.f, s_ml, s_u.acc, s_ticket, [&](float (&acc)[16][kAccRow]) {
+    if constexpr (kShare == 4) {  // the terms' parts together
+#pragma unroll
+      for (int p = 0; p < kSums; ++p) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) O[p][r] += dpp_f<0x128>(O[p][r]);  // row_ror:8
+      }
+    }
+    if (qi % kHeads >= group || second) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* row = &acc[qi % kHeads][NE * (4 * c4 + r)];
+      if constexpr (kShare == 1) {
+#pragma unroll
+        for (int u = 0; u < NE / 4; ++u) *reinterpret_cast<f32x4*>(row + 4 * u) = f32x4{O[4 * u][r], O[4 * u + 1][r], O[4 * u + 2][r], O[4 * u + 3][r]};
+      } else {
+#pragma unroll
+        for (int p = 0; p < kSums; ++p) row[2 * p + (odd ? 1 : 0)] = O[p][r];
+      }
+    }
+  });
 }
 
 template <class Elt, int D, PagedKind kKind>
 int run_fp4(const PagedArgs& base, const PagedPlan& p, const uint32_t* table, hipStream_t stream) {
   const dim3 grid((unsigned)base.heads, (unsigned)p.rows);
+  auto start = [&](const auto& a) {
+    using Args = std::decay_t<decltype(a)>;
+    if (a.group > 8) hipLaunchKernelGGL((fp4_kernel<Elt, D, kKind, 1, Args>), grid, dim3(kThreads), 0, stream, a);
+    else if (a.group > 4) hipLaunchKernelGGL((fp4_kernel<Elt, D, kKind, 2, Args>), grid, dim3(kThreads), 0, stream, a);
+    else hipLaunchKernelGGL((fp4_kernel<Elt, D, kKind, 4, Args>), grid, dim3(kThreads), 0, stream, a);
+    return launched();
+  };
   if constexpr (kKind == kPagedSpans) {
     if (p.table) {
       PagedArgsTable a;
       static_cast<PagedArgs&>(a) = base;
       for (int32_t i = 0; i < p.rows; ++i) a.table[i] = table[i];
-      hipLaunchKernelGGL((fp4_kernel<Elt, D, kKind, PagedArgsTable>), grid, dim3(kThreads), 0, stream, a);
-      return launched();
+      return start(a);
     }
   }
   PagedArgsPlain a;
   static_cast<PagedArgs&>(a) = base;
-  hipLaunchKernelGGL((fp4_kernel<Elt, D, kKind, PagedArgsPlain>), grid, dim3(kThreads), 0, stream, a);
-  return launched();
+  return start(a);
 }
 
 template <PagedKind kKind>
@@ -434,7 +530,7 @@ int decode_fp4(const span_paged_desc_t* d, const void* q, const void* k, const v
   PagedArgs a;
   PagedPlan p;
   uint32_t table[kMaxPlanSlices];
-  const int rc = one_token_args(d, kKind, q, k, v, block_table, ctx_lens, offsets, starts, ends, nullptr, scale, nullptr, out, &a, &p, table);
+  const int rc = one_token_args(d, kKind, q, k, v, block_table, ctx_lens, offsets, starts, ends, nullptr, scale, nullptr, out, &a, &p, table, true);
   if (rc != SPAN_OK) return rc;
   hipStream_t stream = (hipStream_t)d->stream;
   const bool d128 = d->head_dim == 128;

@@ -34,9 +34,9 @@ constexpr int64_t kPagedWorkgroups = 512, kPagedMoreWorkgroups = 1024;
 // heads each, 115.5 -> 110.7.
 constexpr int64_t kPagedOwnWeights = 3 << 19;
 
-PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table) {
+PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table, bool fp4) {
   PagedPlan p = {0, 1, false, 0, false, false};
-  const int64_t cap = capacity(d), whole = paged_whole(d);
+  const int64_t cap = capacity(d), whole = paged_whole(d, fp4), least = paged_least(fp4);
   const int64_t room = std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads), more_room = std::max<int64_t>(1, kPagedMoreWorkgroups / d->kv_heads);
   auto uniform = [&](int64_t splits) {
     splits = std::min(splits, ceil_div(cap, kPagedSliceStep));
@@ -56,7 +56,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table
     if (most <= whole) return uniform(1);
     p.room = (int32_t)room;
     p.splits = 2;
-    p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(most, kPagedLeastSlice) * d->batch));
+    p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(most, least) * d->batch));
     p.cut = more_room > d->batch;  // (otherwise one slice each whatever the lengths; the workspace is that of other batches of the shape)
     p.own_weights = !p.cut && most * d->batch * d->kv_heads <= kPagedOwnWeights;
     return p;
@@ -74,7 +74,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table
       const int64_t most = std::min<int64_t>(aim, kMaxPlanSlices);
       T = longest;
       if (most > d->batch) {
-        T = std::max<int64_t>(kPagedLeastSlice, round_up(2 * sum / (2 * most - d->batch), kPagedSliceStep));
+        T = std::max<int64_t>(least, round_up(2 * sum / (2 * most - d->batch), kPagedSliceStep));
         while (T < longest) {
           int64_t total = 0;
           for (int32_t b = 0; b < d->batch; ++b) total += slices(b);
@@ -82,7 +82,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table
           T = std::min(std::max(round_up(T * total / most, kPagedSliceStep), round_up(T + T / 16, kPagedSliceStep)), longest);
         }
       }
-      if (std::min(T, longest) * std::max<int64_t>(most, d->batch) * 5 <= 7 * sum || T <= kPagedLeastSlice) break;
+      if (std::min(T, longest) * std::max<int64_t>(most, d->batch) * 5 <= 7 * sum || T <= least) break;
     }
     int64_t most = 1, least = kMaxPlanSplits, y = 0;
     for (int32_t b = 0; b < d->batch; ++b) {
@@ -106,7 +106,7 @@ PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table
       return p;
     }
   }
-  return uniform(std::min(ceil_div(room, d->batch), ceil_div(cap, kPagedLeastSlice)));
+  return uniform(std::min(ceil_div(room, d->batch), ceil_div(cap, least)));
 }
 
 PagedWorkspace paged_workspace(const span_paged_desc_t* d, const PagedPlan& p, PagedKind kind, bool weights) {
@@ -211,7 +211,7 @@ extern "C" size_t paged_workspace_bytes(const span_paged_desc_t* desc, int use) 
   if (use == PAGED_SELECTED_DECODE && desc->budget < 1) return 0;
   if (use >= PAGED_SELECTED_DECODE && use <= PAGED_SPAN_DECODE_FP4) {
     const PagedKind kind = use == PAGED_SELECTED_DECODE ? kPagedSelected : use == PAGED_DECODE_FP4 ? kPagedDense : kPagedSpans;
-    return paged_workspace(desc, plan_paged(desc, kind, nullptr), kind, false).total;
+    return paged_workspace(desc, plan_paged(desc, kind, nullptr, use != PAGED_SELECTED_DECODE), kind, false).total;
   }
   if (use < PAGED_DECODE || use > PAGED_SPAN_DECODE_WEIGHTS) return 0;
   const bool spans = use >= PAGED_SPAN_DECODE;

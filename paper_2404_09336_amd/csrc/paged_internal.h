@@ -15,7 +15,10 @@ constexpr int kPagedLeastSlice = 128;  // do not cut finer: a tile per wave
 constexpr int kPagedLocateBatch = 512;
 
 // A sequence of up to so many positions is not cut: the hand-over costs more than a workgroup's two or four tiles a wave.
-inline int32_t paged_whole(const span_paged_desc_t* d) { return d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
+inline int32_t paged_whole(const span_paged_desc_t* d, bool fp4) { return fp4 ? 1024 : d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
+// Rows of 4 bits are through four times as fast, and a hand-over (some 3.5 us) costs as much as a thousand of them.  us, 256 positions at least and whole up to 256 -> 512 and 1024: 16 x 32
+// pairs of ~500 in spans 15.6 -> 14.1; 64 x 8 of 512 .. 4096 and 4 x 8 of 8000 .. 32768 the same.
+inline int32_t paged_least(bool fp4) { return fp4 ? 512 : kPagedLeastSlice; }
 
 int check_paged(const span_paged_desc_t* d);
 
@@ -38,7 +41,8 @@ struct PagedPlan {
   bool own_weights;  // the workgroup that attends adds up the weights too
 };
 // `table` (kMaxPlanSlices entries) may be null to only size the plan.
-PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table);
+// (fp4: of a cache held in 4 bits)
+PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table, bool fp4 = false);
 inline PagedPlan plan_paged(const span_paged_desc_t* d, bool spans, uint32_t* table) { return plan_paged(d, spans ? kPagedSpans : kPagedDense, table); }
 
 // Parts of the workspace of a one-token call, in bytes from its start.
