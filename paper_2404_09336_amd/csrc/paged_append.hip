@@ -24,7 +24,7 @@ struct TurnArgs : TokenArgs {
   const float* angles;       // [angle_rows, channels]: cosines, sines
   int32_t angle_rows, channels;  // channels 0: nothing is turned
   int32_t heads, kv_heads;
-  int32_t kv_chunks, q_chunks;   // waves that a token's rows of K (as many of V), and of q, take
+  int32_t chunks;                // waves that a token's rows take: those of K, then of V, then of q
 };
 
 struct ReadArgs : TokenArgs {
@@ -32,11 +32,13 @@ struct ReadArgs : TokenArgs {
   const unsigned char* v;
   u32x4* k_rows;
   u32x4* v_rows;
-  int32_t kv_heads, kv_chunks;
+  int32_t kv_heads, chunks;
 };
 
-constexpr int kTurnLoads = 4;  // pieces of 16 bytes per lane
-constexpr int kTurnPieces = 64 * kTurnLoads;
+// A wave takes a chunk of so many pieces of 16 bytes per lane of one token's rows; a workgroup's waves the same chunk of neighbouring tokens, or neighbouring chunks.
+constexpr int kFewLoads = 2, kManyLoads = 12, kFp4Loads = 4;
+constexpr int kWaves = 4, kFp4Waves = 16;  // (sixteen tokens' rows of 4-bit values fill their lines together, in one L2)
+constexpr int32_t kManyTokens = 512;
 
 // The sequence of a token's row, its slot and true position; b < 0: it belongs to none.
 struct Token {
@@ -81,12 +83,13 @@ template <class Elt, bool kPaired>
 struct Angles {
   static constexpr int kPer = Elt::kPerVec, kOwn = kPaired ? kPer / 2 : kPer;
   float cosine[kOwn], sine[kOwn];
-  int partner;  // halves: pieces from a lane's to that of the other channels
+  int partner;  // halves: lanes from a lane's piece to that of the other channels
   bool turned;
 
   __device__ __forceinline__ void load(const TurnArgs& a, int position, int piece) {
     const int d = piece * kPer, half = a.channels / 2;
     turned = d < a.channels;
+    partner = 0;
     if (!turned) return;
     const bool second = !kPaired && d >= half;
     const int first = kPaired ? d / 2 : d - (second ? half : 0);
@@ -128,16 +131,16 @@ __device__ __forceinline__ float to_odd(double x) {
 }
 // The same as turn, to the odd neighbour of the exact value: products of two fp32 are exact in 64 bits, their sum is rounded once.
 template <class Elt, bool kPaired>
-__device__ __forceinline__ void turn_exactly(const Angles<Elt, kPaired>& g, float* x, const float* other) {
+__device__ __forceinline__ void turn_exactly(const double* cosine, const double* sine, float* x, const float* other) {
 #pragma unroll
   for (int i = 0; i < Elt::kPerVec; ++i) {
     if constexpr (kPaired) {
       if (i & 1) continue;
-      const double one = x[i], two = x[i + 1], c = g.cosine[i / 2], s = g.sine[i / 2];
+      const double one = x[i], two = x[i + 1], c = cosine[i / 2], s = sine[i / 2];
       x[i] = to_odd(fma(one, c, -(two * s)));
       x[i + 1] = to_odd(fma(one, s, two * c));
     } else {
-      x[i] = to_odd(fma((double)x[i], (double)g.cosine[i], (double)other[i] * (double)g.sine[i]));
+      x[i] = to_odd(fma((double)x[i], cosine[i], (double)other[i] * sine[i]));
     }
   }
 }
@@ -186,137 +189,147 @@ __device__ __forceinline__ uint32_t exponent_at(uint32_t page_rows, uint32_t row
   return page_rows * (D / 2u) + row / kFp4Rows * (D / 2u) + c / 32u * 16u + row % kFp4Rows;
 }
 
-// A wave takes up to 4 KB of one token's rows of K, of V, or of q.  Bound by memory where there are many rows, by the chain of trips (offsets, length, page) where there are few.
-template <class Elt, int D, bool kFp4, bool kPaired>
-__global__ __launch_bounds__(256) void turn_kernel(const TurnArgs a) {
+// Bound by memory where there are many rows, by the chain of trips (offsets, length, angles and page) where there are few.
+template <class Elt, int D, bool kFp4, bool kPaired, int kLoads>
+__global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(const TurnArgs a) {
   constexpr int kPer = Elt::kPerVec, kRow = D / kPer;  // pieces of a row
+  constexpr int kChunk = 64 * kLoads;
   const int lane = threadIdx.x & 63;
-  const uint32_t unit = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4u + (threadIdx.x >> 6)));
-  const uint32_t chunks = 2u * (uint32_t)a.kv_chunks + (uint32_t)a.q_chunks;
-  const int t = (int)(unit / chunks);
-  int c = (int)(unit % chunks);
+  const uint32_t chunks = (uint32_t)a.chunks, waves = blockDim.x >> 6, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const uint32_t unit = blockIdx.x * waves + wave;
+  const int t = kFp4 ? (int)(blockIdx.x / chunks * waves + wave) : (int)(unit / chunks), c = kFp4 ? (int)(blockIdx.x % chunks) : (int)(unit % chunks);
   if (t >= a.num_tokens) return;
-  const bool is_k = c < a.kv_chunks, is_v = !is_k && c < 2 * a.kv_chunks;
-  c -= is_k ? 0 : is_v ? a.kv_chunks : 2 * a.kv_chunks;
-  const int pieces = (is_k || is_v ? a.kv_heads : a.heads) * kRow;
-  const u32x4* from = (is_k ? a.k_new : is_v ? a.v_new : a.q) + (size_t)t * pieces;
-  const int first = c * kTurnPieces + lane, piece = first % kRow;
-  u32x4 x[kTurnLoads], other[kTurnLoads];
+  const int rows = 2 * a.kv_heads + (a.q != nullptr ? a.heads : 0), pieces = rows * kRow;
+  const int first = c * kChunk + lane, piece = lane % kRow;
+  // Row number `row` of a token: of K, of V or of q, where it begins.
+  auto source = [&](int row) {
+    const bool is_q = row >= 2 * a.kv_heads, is_v = row >= a.kv_heads;
+    const u32x4* of = is_q ? a.q : is_v ? a.v_new : a.k_new;
+    const int heads = is_q ? a.heads : a.kv_heads, h = row - (is_q ? 2 * a.kv_heads : is_v ? a.kv_heads : 0);
+    return of + ((size_t)t * (size_t)heads + (size_t)h) * (size_t)kRow;
+  };
+  auto whole_or_part = [&](auto whole) {  // (a whole chunk's loads are not parted by branches)
+    constexpr bool kWhole = decltype(whole)::value;
+    u32x4 x[kLoads];
 #pragma unroll
-  for (int i = 0; i < kTurnLoads; ++i) x[i] = from[min(first + 64 * i, pieces - 1)];
-  const bool turns = !is_v && a.channels > 0;
-  const Token tok = find_token(a, t, lane);
-  if (tok.b < 0) return;
-  Angles<Elt, kPaired> g;
-  g.turned = false;
-  g.partner = 0;
-  if (turns) g.load(a, tok.position, piece);
-  if (!kPaired && turns) {
-#pragma unroll
-    for (int i = 0; i < kTurnLoads; ++i) {
-      const int at = min(first + 64 * i, pieces - 1);
-      other[i] = from[g.turned && first + 64 * i < pieces ? at + g.partner : at];
+    for (int i = 0; i < kLoads; ++i) {
+      if (!kWhole && c * kChunk + 64 * i >= pieces) break;
+      const int at = kWhole ? first + 64 * i : min(first + 64 * i, pieces - 1);
+      x[i] = __builtin_nontemporal_load(source(at / kRow) + piece);
     }
-  }
-  if (is_k && c == 0 && a.positions != nullptr && (uint32_t)tok.p < (uint32_t)a.max_len) {
-    for (int h = lane; h < a.kv_heads; h += 64) a.positions[((size_t)tok.b * a.kv_heads + h) * (size_t)a.max_len + tok.p] = tok.position;
-  }
-  int row = -1;
-  if (is_k || is_v) {
-    row = token_row(a, tok);
-    if (row < 0) return;
-  }
-  const size_t page = (size_t)(max(row, 0) >> a.page_shift);
-  const uint32_t page_rows = 1u << a.page_shift, in_page = (uint32_t)max(row, 0) & (page_rows - 1u);
-#pragma unroll
-  for (int i = 0; i < kTurnLoads; ++i) {
-    const int at = first + 64 * i;
-    float f[kPer];
-    const bool to_fp4 = kFp4 && (is_k || is_v);
-    if (to_fp4 || g.turned) {
-      Elt::unpack(x[i], f);
-      if (g.turned) {
-        float o[kPer];
-        if constexpr (!kPaired) Elt::unpack(other[i], o);
-        if (to_fp4) turn_exactly<Elt, kPaired>(g, f, o);
-        else turn<Elt, kPaired>(g, f, o);
-        if (!to_fp4) x[i] = pack_values<Elt>(f);
-      }
-    }
+    const Token tok = find_token(a, t, lane);
+    if (tok.b < 0) return;
+    Angles<Elt, kPaired> g;
+    g.turned = false;
+    g.partner = 0;
+    if (a.channels > 0) g.load(a, tok.position, piece);
+    double cosine[Angles<Elt, kPaired>::kOwn], sine[Angles<Elt, kPaired>::kOwn];
     if constexpr (kFp4) {
-      if (is_k || is_v) {  // (all lanes: a block's are exchanged; the rows of one token end with a whole block)
-        const uint32_t exponent = block_exponent<kPer>(f), w = to_codes<kPer>(f, exponent);
-        if (at < pieces) {
-          const int h = at / kRow;
+#pragma unroll
+      for (int i = 0; i < Angles<Elt, kPaired>::kOwn; ++i) cosine[i] = (double)g.cosine[i], sine[i] = (double)g.sine[i];
+    }
+    if (c == 0 && a.positions != nullptr && (uint32_t)tok.p < (uint32_t)a.max_len) {
+      for (int h = lane; h < a.kv_heads; h += 64) a.positions[((size_t)tok.b * a.kv_heads + h) * (size_t)a.max_len + tok.p] = tok.position;
+    }
+    const int at_row = c * kChunk < 2 * a.kv_heads * kRow ? token_row(a, tok) : -1;  // of the pool (a chunk of q needs none)
+    const size_t page = (size_t)(max(at_row, 0) >> a.page_shift);
+    const uint32_t page_rows = 1u << a.page_shift, in_page = (uint32_t)max(at_row, 0) & (page_rows - 1u);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (!kWhole && c * kChunk + 64 * i >= pieces) break;
+      const int at = first + 64 * i, row = at / kRow;
+      const bool is_q = row >= 2 * a.kv_heads, is_v = !is_q && row >= a.kv_heads;
+      const int h = row - (is_q ? 2 * a.kv_heads : is_v ? a.kv_heads : 0);
+      const bool turned = g.turned && !is_v;
+      float f[kPer], o[kPer];
+      Elt::unpack(x[i], f);
+      if (!kPaired && a.channels > 0) {  // (of every lane: the other channels' values come from theirs)
+        u32x4 other;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) other[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane + g.partner), (int)x[i][k]);
+        Elt::unpack(other, o);
+      }
+      if (kFp4 && !is_q) {
+        if (turned) turn_exactly<Elt, kPaired>(cosine, sine, f, o);
+        const uint32_t exponent = block_exponent<kPer>(f), w = to_codes<kPer>(f, exponent);  // (a block's lanes are all here)
+        if (at_row >= 0 && (kWhole || at < pieces)) {
           const uint32_t ch = (uint32_t)piece * kPer;
-          unsigned char* to = (unsigned char*)(is_k ? a.k : a.v) + (page * (size_t)a.kv_heads + (size_t)h) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
-          if (is_k) {
-            if constexpr (kPer == 8) *(uint32_t*)(to + code_at<D, false>(in_page, ch)) = w;
-            else *(uint16_t*)(to + code_at<D, false>(in_page, ch)) = (uint16_t)w;
-          } else if constexpr (kPer == 8 && D == 128) {
-            *(uint32_t*)(to + code_at<D, true>(in_page, ch)) = w;
+          unsigned char* to = (unsigned char*)(is_v ? a.v : a.k) + (page * (size_t)a.kv_heads + (size_t)h) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
+          const uint32_t code = is_v ? code_at<D, true>(in_page, ch) : code_at<D, false>(in_page, ch);
+          if constexpr (kPer == 8 && D == 128) {
+            *(uint32_t*)(to + code) = w;
+          } else if constexpr (kPer == 8) {
+            *(uint16_t*)(to + code) = (uint16_t)w;
+            *(uint16_t*)(to + (is_v ? code_at<D, true>(in_page, ch + 4u) : code + 2u)) = (uint16_t)(w >> 16);
           } else {
-            *(uint16_t*)(to + code_at<D, true>(in_page, ch)) = (uint16_t)w;
-            if constexpr (kPer == 8) *(uint16_t*)(to + code_at<D, true>(in_page, ch + 4u)) = (uint16_t)(w >> 16);
+            *(uint16_t*)(to + code) = (uint16_t)w;
           }
           if (ch % kFp4Block == 0) to[exponent_at<D>(page_rows, in_page, ch)] = (unsigned char)exponent;
         }
         continue;
       }
-    }
-    if (at < pieces) {
-      if (is_k || is_v) {
-        const size_t to = (((page * (size_t)a.kv_heads + (size_t)(at / kRow)) << a.page_shift) + in_page) * (size_t)kRow + (size_t)piece;
-        ((u32x4*)(is_k ? a.k : a.v))[to] = x[i];
-      } else {
-        a.q_out[(size_t)t * pieces + at] = x[i];
+      if (turned) {
+        turn<Elt, kPaired>(g, f, o);
+        x[i] = pack_values<Elt>(f);
+      }
+      if (!kWhole && at >= pieces) continue;
+      if (is_q) {
+        __builtin_nontemporal_store(x[i], a.q_out + ((size_t)t * (size_t)a.heads + (size_t)h) * (size_t)kRow + (size_t)piece);
+      } else if (!kFp4 && at_row >= 0) {
+        const size_t to = (((page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) + in_page) * (size_t)kRow + (size_t)piece;
+        __builtin_nontemporal_store(x[i], (u32x4*)(is_v ? a.v : a.k) + to);
       }
     }
-  }
+  };
+  if ((c + 1) * kChunk <= pieces) whole_or_part(std::true_type());
+  else whole_or_part(std::false_type());
 }
 
 template <class Elt, int D>
-__global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
+__global__ __launch_bounds__(64 * kFp4Waves) void read_kernel(const ReadArgs a) {
   constexpr int kPer = Elt::kPerVec, kRow = D / kPer;
   const int lane = threadIdx.x & 63;
-  const uint32_t unit = (uint32_t)__builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4u + (threadIdx.x >> 6)));
-  const uint32_t chunks = 2u * (uint32_t)a.kv_chunks;
-  const int t = (int)(unit / chunks);
-  int c = (int)(unit % chunks);
+  const uint32_t chunks = (uint32_t)a.chunks, waves = blockDim.x >> 6;
+  const int c = (int)(blockIdx.x % chunks);
+  const int t = __builtin_amdgcn_readfirstlane((int)(blockIdx.x / chunks * waves + (threadIdx.x >> 6)));
   if (t >= a.num_tokens) return;
-  const bool is_k = c < a.kv_chunks;
-  if (!is_k) c -= a.kv_chunks;
   const Token tok = find_token(a, t, lane);
   if (tok.b < 0) return;
-  const int row = token_row(a, tok);
-  if (row < 0) return;
-  const size_t page = (size_t)(row >> a.page_shift);
-  const uint32_t page_rows = 1u << a.page_shift, in_page = (uint32_t)row & (page_rows - 1u);
-  const int pieces = a.kv_heads * kRow;
+  const int at_row = token_row(a, tok);
+  if (at_row < 0) return;
+  const size_t page = (size_t)(at_row >> a.page_shift);
+  const uint32_t page_rows = 1u << a.page_shift, in_page = (uint32_t)at_row & (page_rows - 1u);
+  const int pieces = 2 * a.kv_heads * kRow, piece = lane % kRow;
+  const uint32_t ch = (uint32_t)piece * kPer;
+  uint32_t w[kFp4Loads], exponent[kFp4Loads];
 #pragma unroll
-  for (int i = 0; i < kTurnLoads; ++i) {
-    const int at = c * kTurnPieces + lane + 64 * i;
-    if (at >= pieces) continue;
-    const uint32_t ch = (uint32_t)(at % kRow) * kPer;
-    const unsigned char* of = (is_k ? a.k : a.v) + (page * (size_t)a.kv_heads + (size_t)(at / kRow)) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
-    const float scale = __builtin_bit_cast(float, (uint32_t)of[exponent_at<D>(page_rows, in_page, ch)] << 23);
-    uint32_t w;
-    if (is_k) w = kPer == 8 ? *(const uint32_t*)(of + code_at<D, false>(in_page, ch)) : (uint32_t) * (const uint16_t*)(of + code_at<D, false>(in_page, ch));
-    else if constexpr (kPer == 8 && D == 128) w = *(const uint32_t*)(of + code_at<D, true>(in_page, ch));
-    else {
-      w = *(const uint16_t*)(of + code_at<D, true>(in_page, ch));
-      if constexpr (kPer == 8) w |= (uint32_t) * (const uint16_t*)(of + code_at<D, true>(in_page, ch + 4u)) << 16;
-    }
+  for (int i = 0; i < kFp4Loads; ++i) {
+    const int row = min(c * (64 * kFp4Loads) + lane + 64 * i, pieces - 1) / kRow;
+    const bool is_v = row >= a.kv_heads;
+    const unsigned char* of =
+        (is_v ? a.v : a.k) + (page * (size_t)a.kv_heads + (size_t)(is_v ? row - a.kv_heads : row)) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
+    const uint32_t code = is_v ? code_at<D, true>(in_page, ch) : code_at<D, false>(in_page, ch);
+    exponent[i] = of[exponent_at<D>(page_rows, in_page, ch)];
+    if constexpr (kPer == 8 && D == 128) w[i] = *(const uint32_t*)(of + code);
+    else if constexpr (kPer == 8) w[i] = *(const uint16_t*)(of + code) | (uint32_t) * (const uint16_t*)(of + (is_v ? code_at<D, true>(in_page, ch + 4u) : code + 2u)) << 16;
+    else w[i] = *(const uint16_t*)(of + code);
+  }
+#pragma unroll
+  for (int i = 0; i < kFp4Loads; ++i) {
+    const int at = c * (64 * kFp4Loads) + lane + 64 * i, row = at / kRow;
+    const bool is_v = row >= a.kv_heads;
+    const float scale = __builtin_bit_cast(float, exponent[i] << 23);
     float f[8];
-    f32x2 two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
+    f32x2 two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 0);
     f[0] = two[0], f[1] = two[1];
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 1);
     f[2] = two[0], f[3] = two[1];
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2);
+    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 2);
     f[4] = two[0], f[5] = two[1];
-    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+    two = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[i], scale, 3);
     f[6] = two[0], f[7] = two[1];
-    (is_k ? a.k_rows : a.v_rows)[(size_t)t * pieces + at] = pack_values<Elt>(f);
+    if (at < pieces)
+      (is_v ? a.v_rows : a.k_rows)[((size_t)t * (size_t)a.kv_heads + (size_t)(is_v ? row - a.kv_heads : row)) * (size_t)kRow + (size_t)piece] = pack_values<Elt>(f);
   }
 }
 
@@ -335,23 +348,30 @@ TokenArgs token_args(const span_paged_desc_t* d, const int32_t* block_table, con
   return a;
 }
 
-int32_t chunks_of(const span_paged_desc_t* d, int32_t heads) {
-  const int64_t pieces = (int64_t)heads * (d->head_dim * (d->dtype == SPAN_F32 ? 4 : 2) / 16);
-  return (int32_t)((pieces + kTurnPieces - 1) / kTurnPieces);
+// Chunks of so many loads that `rows` rows of a token take.
+int64_t chunks_of(const span_paged_desc_t* d, int64_t rows, int loads) {
+  const int64_t pieces = rows * (d->head_dim * (d->dtype == SPAN_F32 ? 4 : 2) / 16);
+  return (pieces + 64 * loads - 1) / (64 * loads);
 }
 
-// Workgroups of four waves, one wave for each of so many chunks of a token; false: more than a grid holds.
-bool grid_of(const span_paged_desc_t* d, int64_t chunks, dim3* grid) {
-  const int64_t waves = (int64_t)d->num_tokens * chunks;
-  if (waves > 0x7fffffff) return false;
-  *grid = dim3((unsigned)((waves + 3) / 4));
+struct TokenGrid {
+  dim3 grid, block;
+};
+// Grid of so many waves a token; false: more than it holds.
+bool grid_of(const span_paged_desc_t* d, int64_t chunks, int waves, TokenGrid* g) {
+  const int64_t groups = ((int64_t)d->num_tokens + waves - 1) / waves * chunks;
+  if (groups * waves > 0x7fffffff) return false;
+  g->grid = dim3((unsigned)groups);
+  g->block = dim3((unsigned)(64 * waves));
   return true;
 }
 
 template <class Elt, int D, bool kFp4>
-void start_turn(const TurnArgs& a, bool paired, dim3 grid, hipStream_t stream) {
-  if (paired) hipLaunchKernelGGL((turn_kernel<Elt, D, kFp4, true>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((turn_kernel<Elt, D, kFp4, false>), grid, dim3(256), 0, stream, a);
+void start_turn(const TurnArgs& a, bool paired, bool many, const TokenGrid& g, hipStream_t stream) {
+  constexpr int kMany = kFp4 ? kFp4Loads : kManyLoads;
+  auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, g.grid, g.block, 0, stream, a); };
+  if (many) paired ? start(turn_kernel<Elt, D, kFp4, true, kMany>) : start(turn_kernel<Elt, D, kFp4, false, kMany>);
+  else paired ? start(turn_kernel<Elt, D, kFp4, true, kFewLoads>) : start(turn_kernel<Elt, D, kFp4, false, kFewLoads>);
 }
 
 template <bool kFp4>
@@ -384,21 +404,22 @@ int append_turned(const span_paged_desc_t* d, const paged_rotation_t* rotation, 
   }
   a.heads = d->heads;
   a.kv_heads = d->kv_heads;
-  a.kv_chunks = chunks_of(d, d->kv_heads);
-  a.q_chunks = q ? chunks_of(d, d->heads) : 0;
-  dim3 grid;
-  if (!grid_of(d, 2 * (int64_t)a.kv_chunks + a.q_chunks, &grid)) return SPAN_ERR_SHAPE;
+  const bool many = d->num_tokens >= kManyTokens;
+  const int64_t chunks = chunks_of(d, 2 * (int64_t)d->kv_heads + (q ? d->heads : 0), !many ? kFewLoads : kFp4 ? kFp4Loads : kManyLoads);
+  TokenGrid grid;
+  if (!grid_of(d, chunks, kFp4 && many ? kFp4Waves : kWaves, &grid)) return SPAN_ERR_SHAPE;
+  a.chunks = (int32_t)chunks;
   const bool paired = rotation && rotation->paired, d128 = d->head_dim == 128;
   hipStream_t stream = (hipStream_t)d->stream;
   switch (d->dtype) {
     case SPAN_F32:
-      d128 ? start_turn<F32, 128, kFp4>(a, paired, grid, stream) : start_turn<F32, 64, kFp4>(a, paired, grid, stream);
+      d128 ? start_turn<F32, 128, kFp4>(a, paired, many, grid, stream) : start_turn<F32, 64, kFp4>(a, paired, many, grid, stream);
       break;
     case SPAN_F16:
-      d128 ? start_turn<F16, 128, kFp4>(a, paired, grid, stream) : start_turn<F16, 64, kFp4>(a, paired, grid, stream);
+      d128 ? start_turn<F16, 128, kFp4>(a, paired, many, grid, stream) : start_turn<F16, 64, kFp4>(a, paired, many, grid, stream);
       break;
     default:
-      d128 ? start_turn<BF16, 128, kFp4>(a, paired, grid, stream) : start_turn<BF16, 64, kFp4>(a, paired, grid, stream);
+      d128 ? start_turn<BF16, 128, kFp4>(a, paired, many, grid, stream) : start_turn<BF16, 64, kFp4>(a, paired, many, grid, stream);
   }
   return launched();
 }
@@ -433,12 +454,13 @@ extern "C" int paged_read_fp4(const span_paged_desc_t* desc, const void* k_pages
   a.k_rows = (u32x4*)k_rows;
   a.v_rows = (u32x4*)v_rows;
   a.kv_heads = desc->kv_heads;
-  a.kv_chunks = chunks_of(desc, desc->kv_heads);
-  dim3 grid;
-  if (!grid_of(desc, 2 * (int64_t)a.kv_chunks, &grid)) return SPAN_ERR_SHAPE;
+  const int64_t chunks = chunks_of(desc, 2 * (int64_t)desc->kv_heads, kFp4Loads);
+  TokenGrid grid;
+  if (!grid_of(desc, chunks, desc->num_tokens >= kManyTokens ? kFp4Waves : kWaves, &grid)) return SPAN_ERR_SHAPE;
+  a.chunks = (int32_t)chunks;
   const bool d128 = desc->head_dim == 128;
   hipStream_t stream = (hipStream_t)desc->stream;
-  auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
+  auto start = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid.grid, grid.block, 0, stream, a); };
   switch (desc->dtype) {
     case SPAN_F32:
       d128 ? start(read_kernel<F32, 128>) : start(read_kernel<F32, 64>);
