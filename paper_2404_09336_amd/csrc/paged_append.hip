@@ -120,27 +120,34 @@ __device__ __forceinline__ void turn(const Angles<Elt, kPaired>& g, float* x, co
   }
 }
 
-// x to fp32, inexact values to the neighbour with an odd last bit: rounded again to fewer bits, with ties to even, it becomes what x would.
+// x to fp32, inexact values to the neighbour with an odd last bit: rounded again to fewer bits, with ties to even, it becomes what x would.  kTiny: also below 2^-126, where
+// fp32 has fewer bits than the 24 that are kept otherwise.
+template <bool kTiny>
 __device__ __forceinline__ float to_odd(double x) {
-  const float f = (float)x;
-  const double back = (double)f;
-  uint32_t u = __builtin_bit_cast(uint32_t, f);
-  if (fabs(back) > fabs(x)) u -= 1u;
-  if (back != x) u |= 1u;
-  return __builtin_bit_cast(float, u);
+  if constexpr (kTiny) {
+    const float f = (float)x;
+    const double back = (double)f;
+    uint32_t u = __builtin_bit_cast(uint32_t, f);
+    if (fabs(back) > fabs(x)) u -= 1u;
+    if (back != x) u |= 1u;
+    return __builtin_bit_cast(float, u);
+  }
+  u32x2 u = __builtin_bit_cast(u32x2, x);
+  u[0] = (u[0] & 0xe0000000u) | min(u[0] & 0x1fffffffu, 1u) << 29;
+  return (float)__builtin_bit_cast(double, u);
 }
 // The same as turn, to the odd neighbour of the exact value: products of two fp32 are exact in 64 bits, their sum is rounded once.
-template <class Elt, bool kPaired>
-__device__ __forceinline__ void turn_exactly(const double* cosine, const double* sine, float* x, const float* other) {
+template <class Elt, bool kPaired, bool kTiny>
+__device__ __forceinline__ void turn_exactly(const Angles<Elt, kPaired>& g, float* x, const float* other) {
 #pragma unroll
   for (int i = 0; i < Elt::kPerVec; ++i) {
     if constexpr (kPaired) {
       if (i & 1) continue;
-      const double one = x[i], two = x[i + 1], c = cosine[i / 2], s = sine[i / 2];
-      x[i] = to_odd(fma(one, c, -(two * s)));
-      x[i + 1] = to_odd(fma(one, s, two * c));
+      const double one = x[i], two = x[i + 1], c = g.cosine[i / 2], s = g.sine[i / 2];
+      x[i] = to_odd<kTiny>(fma(one, c, -(two * s)));
+      x[i + 1] = to_odd<kTiny>(fma(one, s, two * c));
     } else {
-      x[i] = to_odd(fma((double)x[i], cosine[i], (double)other[i] * sine[i]));
+      x[i] = to_odd<kTiny>(fma((double)x[i], (double)g.cosine[i], (double)other[i] * (double)g.sine[i]));
     }
   }
 }
@@ -148,9 +155,10 @@ __device__ __forceinline__ void turn_exactly(const double* cosine, const double*
 // Exponent byte of the block of 32 channels that kLanes lanes hold together, by the largest magnitude (as bits: NaN above infinity above numbers).
 template <int kPer>
 __device__ __forceinline__ uint32_t block_exponent(const float* x) {
-  uint32_t most = 0;
+  float largest = 0.f;  // (NaN stays)
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) most = max(most, __builtin_bit_cast(uint32_t, x[i]) & 0x7fffffffu);
+  for (int i = 0; i < kPer; ++i) largest = __builtin_elementwise_maximum(largest, fabsf(x[i]));
+  uint32_t most = __builtin_bit_cast(uint32_t, largest) & 0x7fffffffu;
   most = max(most, (uint32_t)dpp_i<0xB1>((int)most));            // quad_perm [1,0,3,2]
   most = max(most, (uint32_t)dpp_i<0x4E>((int)most));            // quad_perm [2,3,0,1]
   if (kPer == 4) most = max(most, (uint32_t)dpp_i<0x141>((int)most));  // row_half_mirror
@@ -222,12 +230,8 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
     Angles<Elt, kPaired> g;
     g.turned = false;
     g.partner = 0;
-    if (a.channels > 0) g.load(a, tok.position, piece);
-    double cosine[Angles<Elt, kPaired>::kOwn], sine[Angles<Elt, kPaired>::kOwn];
-    if constexpr (kFp4) {
-#pragma unroll
-      for (int i = 0; i < Angles<Elt, kPaired>::kOwn; ++i) cosine[i] = (double)g.cosine[i], sine[i] = (double)g.sine[i];
-    }
+    const bool only_v = c * kChunk >= a.kv_heads * kRow && (c + 1) * kChunk <= 2 * a.kv_heads * kRow;
+    if (a.channels > 0 && !only_v) g.load(a, tok.position, piece);
     if (c == 0 && a.positions != nullptr && (uint32_t)tok.p < (uint32_t)a.max_len) {
       for (int h = lane; h < a.kv_heads; h += 64) a.positions[((size_t)tok.b * a.kv_heads + h) * (size_t)a.max_len + tok.p] = tok.position;
     }
@@ -243,15 +247,20 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
       const bool turned = g.turned && !is_v;
       float f[kPer], o[kPer];
       Elt::unpack(x[i], f);
-      if (!kPaired && a.channels > 0) {  // (of every lane: the other channels' values come from theirs)
+      if (!kPaired && a.channels > 0 && !only_v) {  // (of every lane: the other channels' values come from theirs)
         u32x4 other;
 #pragma unroll
         for (int k = 0; k < 4; ++k) other[k] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (lane + g.partner), (int)x[i][k]);
         Elt::unpack(other, o);
       }
       if (kFp4 && !is_q) {
-        if (turned) turn_exactly<Elt, kPaired>(cosine, sine, f, o);
-        const uint32_t exponent = block_exponent<kPer>(f), w = to_codes<kPer>(f, exponent);  // (a block's lanes are all here)
+        if (turned) turn_exactly<Elt, kPaired, false>(g, f, o);
+        uint32_t exponent = block_exponent<kPer>(f);  // (a block's lanes are all here)
+        if (turned && exponent == kFp4LeastExponent + 127) {
+          Elt::unpack(x[i], f);
+          turn_exactly<Elt, kPaired, true>(g, f, o);
+        }
+        const uint32_t w = to_codes<kPer>(f, exponent);
         if (at_row >= 0 && (kWhole || at < pieces)) {
           const uint32_t ch = (uint32_t)piece * kPer;
           unsigned char* to = (unsigned char*)(is_v ? a.v : a.k) + (page * (size_t)a.kv_heads + (size_t)h) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
