@@ -203,15 +203,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   const size_t page_stride = page_bytes * (size_t)kv_heads;
   const uint32_t exps_at = (uint32_t)(D / 2) << a.page_shift;
 
-  // The wave's units from its unit w0 on, one per lane: unit of the pool (page * units of a page + unit in the page) and mask of the rows that take part.
-  int held_unit = 0, held_at = 0;
-  uint32_t held_mask = 0;
-  auto find_units = [&](int w0) {
+  // A wave's units, 64 at a time, one per lane: the page of the sequence that holds it, read from the table, its number on the page, and the mask of the rows that take part.
+  struct Found {
+    int page, at;
+    uint32_t mask;
+  };
+  auto find_units = [&](int w0) {  // from the wave's unit w0 on
     const int w = w0 + lane, s = step0 + wave + w / kStepUnits * kWavesPerBlock;
     const int v = s * kStepUnits + w % kStepUnits;  // among the sequence's units
     const bool mine = w / kStepUnits < steps && v < all;
-    int u = -1;
-    held_mask = 0;
+    int u = 0;
+    Found f = {-1, 0, 0u};
     if constexpr (kSpans) {
       int before = 0;
       for (int i0 = 0; i0 < intervals; i0 += 64) {
@@ -225,28 +227,31 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
           if (__shfl(incl, at + step - 1) + before <= v) at += step;
         }
         const int total = __builtin_amdgcn_readlane(incl, 63);
-        const int ex = __shfl(incl - n, at & 63), f = __shfl(from, at & 63), t = __shfl(to, at & 63);
+        const int ex = __shfl(incl - n, at), begin = __shfl(from, at), end = __shfl(to, at);
         if (mine && v >= before && v < before + total) {
-          u = f / kUnitRows + (v - before - ex);
-          held_mask = unit_mask(u, f, t);
+          u = begin / kUnitRows + (v - before - ex);
+          f.mask = unit_mask(u, begin, end);
         }
         before = min(before + total, most_units(a, intervals));
       }
     } else {
       const bool sink = v < seen.first;
       u = sink ? v : v - seen.first + seen.low / kUnitRows;
-      if (mine) held_mask = unit_mask(u, sink ? 0 : seen.low, sink ? seen.sinks : seen.held);
+      if (mine) f.mask = unit_mask(u, sink ? 0 : seen.low, sink ? seen.sinks : seen.held);
     }
-    held_unit = -1;
-    if (mine && held_mask != 0) {
-      held_unit = table[u >> unit_shift];  // the page, until take_units
-      held_at = u & ((1 << unit_shift) - 1);
+    if (mine && f.mask != 0) {
+      f.page = table[u >> unit_shift];
+      f.at = u & ((1 << unit_shift) - 1);
     }
+    return f;
   };
-  auto take_units = [&]() {
-    const bool there = (uint32_t)held_unit < (uint32_t)a.num_pages;
-    if (!there) held_mask = 0;
-    held_unit = there ? (held_unit << unit_shift) + held_at : 0;  // (none: the pool's first, which nobody attends)
+  // Units of the pool (page * units of a page + unit in the page); none: the pool's first, which nobody attends.
+  int held_unit = 0;
+  uint32_t held_mask = 0;
+  auto hold = [&](const Found& f) {
+    const bool there = (uint32_t)f.page < (uint32_t)a.num_pages;
+    held_mask = there ? f.mask : 0u;
+    held_unit = there ? (f.page << unit_shift) + f.at : 0;
   };
 
   float ref = -INFINITY, lsum = 0.f;
@@ -446,10 +451,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
     }
   };
 
-  if (steps > 0) find_units(0);
+  const Found first_units = find_units(0);
   if (tid < q_parts) q_block0.lay(a, tid, s_u.q);  // (while the table's entries are on their way)
   if (steps > 0) {
-    take_units();
+    hold(first_units);
     fetch(0, std::integral_constant<int, 0>());
   }
   for (int i = tid + kThreads; i < q_parts; i += kThreads) {
@@ -462,10 +467,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   const int units = steps * kStepUnits;
   auto next_of = [&](int w) {
     const int next = w + kStepUnits;
-    if (next < units && next % kHeldUnits == 0) {
-      find_units(next);
-      take_units();
-    }
+    if (next < units && next % kHeldUnits == 0) hold(find_units(next));
     return next;
   };
   for (int w = 0; w < units; w += 2 * kStepUnits) {
