@@ -174,15 +174,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
 
   SeenUnits seen = {0, 0, 0, 0};
   int first_interval = 0, intervals = 0, all;  // units of the sequence
+  struct Interval {
+    int from, to, units;
+  };
+  Interval first_chunk = {0, 0, 0};  // of the sequence's first 64 intervals this lane's
+  auto interval_of = [&](int i0) {   // of the 64 from i0 on
+    Interval v = {0, 0, 0};
+    if (i0 + lane < intervals) v.units = interval_units(a, a.starts[first_interval + i0 + lane], a.ends[first_interval + i0 + lane], v.from, v.to);
+    return v;
+  };
   if constexpr (kSpans) {
     const int lo = clampi(__builtin_amdgcn_readfirstlane(a.offsets[b]), 0, a.num_intervals);
     first_interval = lo;
     intervals = clampi(__builtin_amdgcn_readfirstlane(a.offsets[b + 1]), lo, a.num_intervals) - lo;
     all = 0;
     for (int i0 = 0; i0 < intervals; i0 += 64) {
-      int from, to, n = 0;
-      if (i0 + lane < intervals) n = interval_units(a, a.starts[lo + i0 + lane], a.ends[lo + i0 + lane], from, to);
-      all = min(all + __builtin_amdgcn_readlane(wave_inclusive_scan(n), 63), most_units(a, intervals));
+      const Interval v = interval_of(i0);
+      if (i0 == 0) first_chunk = v;
+      all = min(all + __builtin_amdgcn_readlane(wave_inclusive_scan(v.units), 63), most_units(a, intervals));
     }
   } else {
     if (a.room == 0) sl.len = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]);
@@ -217,8 +226,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
     if constexpr (kSpans) {
       int before = 0;
       for (int i0 = 0; i0 < intervals; i0 += 64) {
-        int from = 0, to = 0, n = 0;
-        if (i0 + lane < intervals) n = interval_units(a, a.starts[first_interval + i0 + lane], a.ends[first_interval + i0 + lane], from, to);
+        const Interval iv = i0 == 0 ? first_chunk : interval_of(i0);
+        const int n = iv.units;
         const int incl = wave_inclusive_scan(n);
         // the first interval whose units end behind v
         int at = 0;
@@ -227,7 +236,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
           if (__shfl(incl, at + step - 1) + before <= v) at += step;
         }
         const int total = __builtin_amdgcn_readlane(incl, 63);
-        const int ex = __shfl(incl - n, at), begin = __shfl(from, at), end = __shfl(to, at);
+        const int ex = __shfl(incl - n, at), begin = __shfl(iv.from, at), end = __shfl(iv.to, at);
         if (mine && v >= before && v < before + total) {
           u = begin / kUnitRows + (v - before - ex);
           f.mask = unit_mask(u, begin, end);

@@ -122,13 +122,36 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
   // pages ahead of `first` and from `last` on are listed in any case
   const int first = min((a.sinks + P - 1) >> a.page_shift, pages), last = max(len - max(a.recent, 1), 0) >> a.page_shift;
 
-  // ---- bounds of pages with new rows: a wave each, row by row --------------------------------------------
+  const bool scored = pages > a.budget, alone = pages <= a.chunk;
+  float* scores = a.scores + bh * (size_t)a.table_pages;
+  auto put_score = [&](int j, float score) {
+    if (alone) s_scores[j] = score;
+    else publish(scores + j, score);
+  };
+  // The lanes of a page's lower half hold the least values, which meet the queries' negative parts, the others the largest and the positive ones.
+  double part[kPer];
+  {
+    const int piece = lane % kRow;
+    const bool upper = lane % kLanes >= kRow;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) part[i] = 0.0;
+    for (int g = 0; g < (scored ? a.group : 0); ++g) {
+      float f[kPer];
+      Elt::unpack(((const u32x4*)a.q)[(bh * (size_t)a.group + (size_t)g) * (size_t)kRow + piece], f);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) part[i] += (double)(upper ? __builtin_elementwise_maximum(f[i], 0.f) : __builtin_elementwise_minimum(f[i], 0.f));
+    }
+  }
+
+  // ---- bounds, and scores, of pages with new rows: a wave each, row by row -------------------------------
   const int fresh0 = max(chunk0, since >> a.page_shift);
   for (int j = fresh0 + wave; j < chunk1; j += kSelectWaves) {
     const int page = __builtin_amdgcn_readfirstlane(table[j]);
-    if ((uint32_t)page >= (uint32_t)a.num_pages) continue;
-    const int row0 = max(since - (j << a.page_shift), 0), row1 = min(len - (j << a.page_shift), P);
-    if (row0 >= row1) continue;
+    if ((uint32_t)page >= (uint32_t)a.num_pages) {
+      if (scored && lane == 0) put_score(j, -INFINITY);
+      continue;
+    }
+    const int row0 = max(since - (j << a.page_shift), 0), row1 = min(len - (j << a.page_shift), P);  // (since = len at the page's end: none)
     constexpr int kRows = 64 / kRow;
     const int piece = lane % kRow;
     const u32x4* rows = a.k + (((size_t)page * (size_t)a.kv_heads + (size_t)h) << a.page_shift) * (size_t)kRow + piece;
@@ -177,39 +200,31 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
       bounds_of(page)[piece] = l;
       bounds_of(page)[kRow + piece] = u;
     }
+    if (scored) {
+      double s = 0.0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) s = fma(part[i], (double)(lane % kLanes >= kRow ? hi[i] : lo[i]), s);
+#pragma unroll
+      for (int apart = 1; apart < kLanes; apart *= 2) s += __shfl_xor(s, apart, 64);
+      if (lane == 0) put_score(j, (float)s);
+    }
   }
 
   int32_t* list = a.selected + bh * (size_t)a.budget;
-  if (pages <= a.budget) {  // all of them
+  if (!scored) {  // all of them
     if (chunk0 == 0) {
       for (int i = tid; i < a.budget; i += kSelectThreads) list[i] = i < pages ? i : -1;
     }
     return;
   }
 
-  // ---- scores --------------------------------------------------------------------------------------------
-  // The lanes of a page's lower half hold the least values, which meet the queries' negative parts, the others the largest and the positive ones.
-  double part[kPer];
-  {
-    const int piece = lane % kRow;
-    const bool upper = lane % kLanes >= kRow;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) part[i] = 0.0;
-    for (int g = 0; g < a.group; ++g) {
-      float f[kPer];
-      Elt::unpack(((const u32x4*)a.q)[(bh * (size_t)a.group + (size_t)g) * (size_t)kRow + piece], f);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) part[i] += (double)(upper ? __builtin_elementwise_maximum(f[i], 0.f) : __builtin_elementwise_minimum(f[i], 0.f));
-    }
-  }
-  if (fresh0 < min(chunk1, last)) __syncthreads();  // new bounds that are scored are written
-  const bool alone = pages <= a.chunk;
-  float* scores = a.scores + bh * (size_t)a.table_pages;
+  // ---- scores of the others -----------------------------------------------------------------------------
+  const int old1 = min(chunk1, fresh0);
   // a group's pages in the first lanes, the next group's on their way
-  auto entry_of = [&](int j0) { return lane < kGroup && j0 + lane < chunk1 ? table[j0 + lane] : -1; };
+  auto entry_of = [&](int j0) { return lane < kGroup && j0 + lane < old1 ? table[j0 + lane] : -1; };
   int j0 = chunk0 + wave * kGroup;
   int entry = entry_of(j0);
-  for (; j0 < chunk1; j0 += kSelectWaves * kGroup) {
+  for (; j0 < old1; j0 += kSelectWaves * kGroup) {
     const uint64_t there = __builtin_amdgcn_ballot_w64((uint32_t)entry < (uint32_t)a.num_pages);
     const int safe = (uint32_t)entry < (uint32_t)a.num_pages ? entry : 0;
     u32x4 x[8];
@@ -227,11 +242,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
     }
     const double sum = sum_of_eight<kLanes>(s, lane);
     const int mine = lane % kLanes / (kLanes / 8) * kAtOnce + lane / kLanes;  // of the group's pages
-    if (lane % (kLanes / 8) == 0 && j0 + mine < chunk1) {
-      const float score = there >> mine & 1u ? (float)sum : -INFINITY;
-      if (alone) s_scores[j0 + mine] = score;
-      else publish(scores + j0 + mine, score);
-    }
+    if (lane % (kLanes / 8) == 0 && j0 + mine < old1) put_score(j0 + mine, there >> mine & 1u ? (float)sum : -INFINITY);
   }
   if (alone) {
     __syncthreads();
