@@ -309,7 +309,7 @@ inline int one_token_args(const span_paged_desc_t* d, PagedKind kind, const void
   a.room = p.cut ? p.room : 0;
   a.more_room = p.rows;
   a.whole = paged_whole(d, fp4);
-  a.least = paged_least(fp4);
+  a.least = paged_least(kind, fp4);
   a.final_ml = weights ? (float*)(at + w.final_ml) : nullptr;
   a.counts = weights && spans ? (int32_t*)(at + w.counts) : nullptr;
   a.list = weights && spans ? (int32_t*)(at + w.list) : nullptr;

@@ -36,7 +36,7 @@ constexpr int64_t kPagedOwnWeights = 3 << 19;
 
 PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table, bool fp4) {
   PagedPlan p = {0, 1, false, 0, false, false};
-  const int64_t cap = capacity(d), whole = paged_whole(d, fp4), least = paged_least(fp4);
+  const int64_t cap = capacity(d), whole = paged_whole(d, fp4), least = paged_least(kind, fp4);
   const int64_t room = std::max<int64_t>(1, kPagedWorkgroups / d->kv_heads), more_room = std::max<int64_t>(1, kPagedMoreWorkgroups / d->kv_heads);
   auto uniform = [&](int64_t splits) {
     splits = std::min(splits, ceil_div(cap, kPagedSliceStep));

@@ -58,8 +58,9 @@ class Fp4Pages:
         digit = np.abs(scale) * (block.reshape(q.shape) @ np.abs(k).transpose(0, 2, 1)) * 2.0 ** -20
         sums = np.abs(scale) * (np.abs(q) @ np.abs(k).transpose(0, 2, 1)) * 2.0 ** -20
         off = np.expm1(2 * (digit + sums).max(-1, keepdims=True))
-        # products with V are exact, their sums round: three a step of 32 positions of a wave, the joins of waves and slices
-        chain = (3 * (len(p) // 32 + 1) + 64) * 2.0 ** -24
+        # A weight goes in as two bf16 terms, each rounded by half a step (2^-9) at most: 2^-18 of it is lost.  Products with V are exact, their sums round: up to three a step of 32
+        # positions of a wave, the joins of waves and slices.
+        chain = 2.0 ** -18 + (3 * (len(p) // 32 + 1) + 64) * 2.0 ** -24
         return (w @ v).reshape(H, D), ((off + chain) * (w @ np.abs(v))).reshape(H, D) + 1e-30
 
 
