@@ -6,12 +6,12 @@
 //     time, and every load is contiguous over the wave.  Where a window, a span or the cache begins or ends inside a unit, its other rows are masked; two intervals that meet in a unit are two units.
 //   * K stays as it is: fp4 x fp6 products with both exponents applied by the matrix core.  q is laid out as kDigits digits to the base 16, each -16 .. 16 times a power of two that 32 channels share:
 //     such a digit is an fp6 value (E2M3) exactly.  (The matrix core adds eight neighbouring products up with some 13 bits below the largest, measured; products of digits fit that, those of
-//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block.
-//   * V becomes bf16, exactly, times its exponent: one instruction for two channels.  Weights meet it as two bf16 terms, each rounded, which together hold 17 bits at least (off by 2^-18 of the weight; a
-//     third would cost a quarter of the step's instructions, for a cache whose values are rounded to two bits).
+//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block, fp32's six 25.
+//   * V becomes bf16, exactly, times its exponent: one instruction for two channels.  Weights meet it as three bf16 terms, all 24 bits.  (Two rounded terms leave 2^-18 of a weight, and outputs
+//     2.4e-6 off in place of 2e-7, for 1 to 3 % of a call.)
 //   * A step of 32 positions is bound by the instructions that a SIMD issues, not by the matrix core, and few heads leave columns free.  With up to 8 heads a head has two columns,
 //     for even and odd channels: its weights go to every other of the product's inner places, zeros between them, and two channels of a row, as the conversion leaves them, need not be parted.  With up to 4
-//     heads it has four, and the two terms go through one product.
+//     heads it has four, and two terms go through one product.
 #include "paged_attend.h"
 
 namespace spanattn {
@@ -31,7 +31,8 @@ constexpr int kStepRows = kUnitRows * kStepUnits;
 constexpr float kSlack = 16.f;
 constexpr int kHeldUnits = 64;                 // of a wave, found at a time: one per lane
 
-constexpr int kDigits = 5;
+template <class Elt>
+constexpr int kDigitsOf = Elt::kBytes == 4 ? 6 : 5;
 
 // Units of a dense call: those of the first `sinks` positions, then those from `low` on.
 struct SeenUnits {
@@ -62,15 +63,16 @@ __device__ __forceinline__ uint32_t unit_mask(int u, int from, int to) {
 }
 
 // q in LDS: of each head and block of 32 channels the fp6 codes of every digit, and the digits' exponent bytes (of digit t byte t).
-template <int D>
+template <class Elt, int D>
 struct DigitTables {
-  uint32_t codes[kDigits][16][D / 32][6];
+  uint32_t codes[kDigitsOf<Elt>][16][D / 32][6];
   uint8_t exps[16][D / 32][8];
 };
 
 // What a thread loads for its (block, digit) number i ...
 template <class Elt, int D>
 struct QueryBlock {
+  static constexpr int kDigits = kDigitsOf<Elt>;
   u32x4 piece[2 * Elt::kBytes];
   __device__ __forceinline__ void load(const PagedArgs& a, size_t row0, int i) {
     const int block = i % (D / 32), j = i / (D / 32 * kDigits);
@@ -79,7 +81,7 @@ struct QueryBlock {
     for (int p = 0; p < 2 * Elt::kBytes; ++p) piece[p] = from[p];
   }
   // ... and the digit's codes.
-  __device__ __forceinline__ void lay(const PagedArgs& a, int i, DigitTables<D>& tab) {
+  __device__ __forceinline__ void lay(const PagedArgs& a, int i, DigitTables<Elt, D>& tab) {
     const int block = i % (D / 32), t = i / (D / 32) % kDigits, j = i / (D / 32 * kDigits);
     float x[32];
 #pragma unroll
@@ -121,15 +123,22 @@ __device__ __forceinline__ f32x4 digit_product(i32x8 k, int k_exp, i32x8 q, u32x
       return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 2, low);
     case 3:
       return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 3, low);
-    default:
+    case 4:
       return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 0, high);
+    default:
+      return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, q, sums, 4, 2, 0, k_exp, 1, high);
   }
 }
 
+// Waves whose registers hold the state, two steps' rows and the weights of one.
+template <int D, int kShare>
+constexpr int kFp4WavesPerSimd = D == 128 && kShare == 1 ? 3 : 4;
+
 // kShare: columns that a query head has, 1, 2 or 4.
 template <class Elt, int D, PagedKind kKind, int kShare, class Args>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))) void fp4_kernel(const Args a) {
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4WavesPerSimd<D, kShare>, kFp4WavesPerSimd<D, kShare>))) void fp4_kernel(const Args a) {
   constexpr bool kSpans = kKind == kPagedSpans;
+  constexpr int kDigits = kDigitsOf<Elt>;
   constexpr int NE = D / 16;              // V channels of a lane
   constexpr int kHeads = 16 / kShare;     // heads that the columns hold
   constexpr int kSums = kShare == 1 ? NE : NE / 2;
@@ -142,7 +151,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   const int h = blockIdx.x, kv_heads = a.heads, group = a.group;
 
   union Overlaid {
-    DigitTables<D> q;
+    DigitTables<Elt, D> q;
     float acc[kWavesPerBlock][16][kAccRow];
   };
   __shared__ __attribute__((aligned(16))) Overlaid s_u;
@@ -166,7 +175,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   const int b = sl.b;
   const size_t bh = (size_t)b * kv_heads + h;
   const int32_t* table = a.block_table + (size_t)b * a.table_pages;
-  const float post = Elt::post_scale(a.scale_log2e);  // weight = exp2((score - largest score) * post)
+  const float post = Elt::post_scale(a.scale_log2e);
 
   const int q_parts = group * (D / 32) * kDigits;  // (block, digit) pairs, a thread's at a time
   QueryBlock<Elt, D> q_block0;
@@ -263,17 +272,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
     held_unit = there ? (f.page << unit_shift) + f.at : 0;
   };
 
-  float ref = -INFINITY, lsum = 0.f;
+  // A weight is exp2(score * post + shift): what the state is relative to is -shift as it is, rounded, and not the score that it came from.
+  float shift = INFINITY, lsum = 0.f;
   // Unnormalised outputs.  kShare 1: O[e][r] of column qi's head, channel NE (4 c4 + r) + e.  Otherwise O[p][r], channel NE (4 c4 + r) + 2 p + odd; kShare 4: the term's part of it.
   f32x4 O[kSums];
 #pragma unroll
   for (int e = 0; e < kSums; ++e) O[e] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int role = qi / kHeads;                    // of the column among its head's
   const bool odd = kShare > 1 && (role & 1);       // the channels that it sums
-  const bool second = kShare == 4 && role >= 2;    // the term that it brings
-  // Selectors of byte permutations: a bf16 value (of two in a dword, by the row's parity) as fp32 for lanes that take the first term away, 0 for the others; its place in the product's operand.
-  const uint32_t sel_first[2] = {kShare == 4 && !second ? 0x0c0c0c0cu : 0x01000c0cu, kShare == 4 && !second ? 0x0c0c0c0cu : 0x03020c0cu};
-  const uint32_t sel_place[2] = {odd ? 0x01000c0cu : 0x0c0c0100u, odd ? 0x03020c0cu : 0x0c0c0302u};
+  const bool second = kShare == 4 && role >= 2;    // the second term's column: it brings the third too, in a product of its own
+  const uint32_t taken = kShare == 4 && !second ? 0u : 0xffff0000u;  // of a weight ahead of the column's first term
+  // Selector of a byte permutation: the upper half of a weight's rest, a bf16 value, to its place in the product's operand, zeros beside it; in columns without a third term, zeros alone.
+  const uint32_t sel_place = odd ? 0x03020c0cu : 0x0c0c0302u, sel_last = kShare == 4 && !second ? 0x0c0c0c0cu : sel_place;
 
   // What a lane holds of a unit.  D = 128: K of row qi, channels 32 c4 on; D = 64: of two units together, K of row qi, unit c4 / 2, channels 32 (c4 % 2) on.  V of rows 4 c4 .. + 3, channels NE qi on.
   // A step's loads are under way while the step before it is worked on.
@@ -385,40 +395,50 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[s][r]);
     }
-    if (__builtin_amdgcn_ballot_w64((mx - ref) * post > kSlack) != 0) {  // (first of all: ref is -infinity)
+    if (__builtin_amdgcn_ballot_w64(fmaf(mx, post, shift) > kSlack) != 0) {
       mx = across_groups_max<16>(mx);
-      const float ref_new = fmaxf(ref, mx), ref_safe = ref_new == -INFINITY ? 0.f : ref_new;
-      const float alpha = __builtin_amdgcn_exp2f((ref - ref_safe) * post);
-      ref = ref_new;
+      const float to = fminf(shift, -(mx * post)), to_safe = to == INFINITY ? 0.f : to;
+      const float alpha = __builtin_amdgcn_exp2f(to_safe - shift);
+      shift = to;
       lsum *= alpha;
 #pragma unroll
       for (int e = 0; e < kSums; ++e) O[e] *= alpha;
     }
-    const float ref_safe = ref == -INFINITY ? 0.f : ref;
-    // Weights as the products' operands, the smaller terms first.  kShare 1: of all 32 rows, two in a dword; otherwise of a unit's, one in a dword.
-    constexpr int kPasses = kShare == 4 ? 1 : 2;
-    u32x4 pairs[2], terms[kPasses][kStepUnits];
+    const float shift_safe = shift == INFINITY ? 0.f : shift;
+    // Weights as the products' operands, the smaller terms first: three times the upper half of what is left, eight bits each.  kShare 1: of all 32 rows, two in a dword; otherwise of a
+    // unit's, one in a dword.
+    constexpr int kPasses = kShare == 4 ? 2 : 3;
+    u32x4 pairs[3], terms[kPasses][kStepUnits];
+    auto less = [](float x, uint32_t mask) { return x - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & mask); };
+    auto upper = [](float x, uint32_t sel) { return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), sel); };
 #pragma unroll
     for (int s = 0; s < kStepUnits; ++s) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) sc[s][r] = __builtin_amdgcn_exp2f((sc[s][r] - ref_safe) * post);
+      for (int r = 0; r < 4; ++r) sc[s][r] = __builtin_amdgcn_exp2f(fmaf(sc[s][r], post, shift_safe));
       lsum += (sc[s][0] + sc[s][1]) + (sc[s][2] + sc[s][3]);
+      if constexpr (kShare == 1) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {  // two rows
-        const uint32_t first = BF16::pack2(sc[s][2 * k], sc[s][2 * k + 1]);
-        float rest[2];
+        for (int k = 0; k < 2; ++k) {
+          float x = sc[s][2 * k], y = sc[s][2 * k + 1];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) rest[r] = sc[s][2 * k + r] - __builtin_bit_cast(float, __builtin_amdgcn_perm(first, first, sel_first[r]));
-        const uint32_t last = BF16::pack2(rest[0], rest[1]);
-        if constexpr (kShare == 1) {
-          pairs[1][2 * s + k] = first;
-          pairs[0][2 * s + k] = last;
-        } else {
-#pragma unroll
-          for (int r = 0; r < 2; ++r) {
-            if constexpr (kShare == 2) terms[1][s][2 * k + r] = __builtin_amdgcn_perm(first, first, sel_place[r]);
-            terms[0][s][2 * k + r] = __builtin_amdgcn_perm(last, last, sel_place[r]);
+          for (int i = 2; i >= 0; --i) {
+            pairs[i][2 * s + k] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, y), __builtin_bit_cast(uint32_t, x), 0x07060302u);
+            x = less(x, 0xffff0000u);
+            y = less(y, 0xffff0000u);
           }
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = sc[s][r];
+          if constexpr (kShare == 2) {
+            terms[kPasses - 1][s][r] = upper(x, sel_place);
+            x = less(x, 0xffff0000u);
+          } else {
+            x = less(x, taken);
+          }
+          terms[1][s][r] = upper(x, sel_place);
+          terms[0][s][r] = upper(less(x, 0xffff0000u), sel_last);
         }
       }
     }
@@ -448,7 +468,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
           const u32x4 v = {__builtin_amdgcn_perm(two[0][1], two[0][0], sel), __builtin_amdgcn_perm(two[0][3], two[0][2], sel),
                            __builtin_amdgcn_perm(two[1][1], two[1][0], sel), __builtin_amdgcn_perm(two[1][3], two[1][2], sel)};
 #pragma unroll
-          for (int i = 0; i < 2; ++i) O[2 * p + k] = BF16::mfma(v, pairs[i], O[2 * p + k]);
+          for (int i = 0; i < 3; ++i) O[2 * p + k] = BF16::mfma(v, pairs[i], O[2 * p + k]);
         }
       } else {
 #pragma unroll
@@ -488,8 +508,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4, 4))
   }
   lsum = across_groups_sum<16>(lsum);
   __syncthreads();  // q's digits are read by all: the states go where they were
-  if (c4 == 0 && qi < kHeads) s_ml[qi][wave] = f32x2{ref, lsum};
-  finish_pair<D, false, kShare>(a, sl, h, post, 1.f, s_ml, s_u.acc, s_ticket, [&](float (&acc)[16][kAccRow]) {
+  if (c4 == 0 && qi < kHeads) s_ml[qi][wave] = f32x2{-shift, lsum};
+  finish_pair<D, false, kShare>(a, sl, h, 1.f, 1.f, s_ml, s_u.acc, s_ticket, [&](float (&acc)[16][kAccRow]) {
     if constexpr (kShare == 4) {  // the terms' parts together
 #pragma unroll
       for (int p = 0; p < kSums; ++p) {

@@ -18,7 +18,7 @@ constexpr int kPagedLocateBatch = 512;
 enum PagedKind { kPagedDense, kPagedSpans, kPagedSelected };
 
 // A sequence of up to so many positions is not cut: the hand-over costs more than a workgroup's two or four tiles a wave.
-inline int32_t paged_whole(const span_paged_desc_t* d, bool fp4) { return fp4 ? 1024 : d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
+inline int32_t paged_whole(const span_paged_desc_t* d, bool fp4 = false) { return fp4 ? 1024 : d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
 // Rows of 4 bits are through four times as fast, and a hand-over (some 3.5 us) costs as much as a thousand of them.  us, 256 positions at least and whole up to 256 -> 512 and 1024: 16 x 32
 // pairs of ~500 in spans 15.6 -> 14.1; 64 x 8 of 512 .. 4096 and 4 x 8 of 8000 .. 32768 the same.
 // Listed pages have a trip more ahead of their rows.  us, 128 -> 256: 4 x 8 pairs of 2048 positions on 32 pages, four query heads each, 13.9 -> 11.9.
