@@ -90,9 +90,10 @@ struct QueryBlock {
       for (int k = 0; k < 4; ++k) piece[p][k] = Elt::scale_query(piece[p][k], a.scale_log2e);
       Elt::unpack(piece[p], x + p * Elt::kPerVec);
     }
-    uint32_t most = 0;
+    float largest = 0.f;  // (NaN stays)
 #pragma unroll
-    for (int k = 0; k < 32; ++k) most = max(most, __builtin_bit_cast(uint32_t, x[k]) & 0x7fffffffu);
+    for (int k = 0; k < 32; ++k) largest = __builtin_elementwise_maximum(largest, fabsf(x[k]));
+    const uint32_t most = __builtin_bit_cast(uint32_t, largest) & 0x7fffffffu;
     // |x| < 2^(e - 126), e the largest's exponent bits; digit t counts 2^(e - 126 - 4 (t + 1)), as an fp6 value 8 times that each
     const int e = max((int)(most >> 23), 1);
     const int scale = e - 126 - 4 * (t + 1) + 3 + 127;
@@ -100,14 +101,15 @@ struct QueryBlock {
     // What the digits ahead of this one leave, x less its nearest multiple of the last one's unit, is the digit times 2^-4 when rounded to a whole number of them: that is how
     // fp6 values up to 2 are spaced.  (Ties fall the same way for all threads.  The conversion takes its values from the two vectors in turn.)
     f32x16 half[2];
+    const float ahead = t == 0 ? 0.f : -1.f;
 #pragma unroll
     for (int k = 0; k < 32; ++k) {
       const float y = __builtin_amdgcn_ldexpf(x[k], 126 - e + 4 * t);
-      half[k % 2][k / 2] = scale < 0 ? 0.f : y - (t == 0 ? 0.f : rintf(y));
+      half[k % 2][k / 2] = fmaf(rintf(y), ahead, y);
     }
     const u32x6 codes = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(half[0], half[1], 0.5f);
 #pragma unroll
-    for (int w = 0; w < 6; ++w) tab.codes[t][j][block][w] = codes[w];
+    for (int w = 0; w < 6; ++w) tab.codes[t][j][block][w] = scale < 0 ? 0u : codes[w];
   }
 };
 
