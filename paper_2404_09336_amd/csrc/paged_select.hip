@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
   constexpr int kLanes = 2 * kRow;                     // of a page's bounds: 16, 32 or 64
   constexpr int kAtOnce = 64 / kLanes;                 // pages of one load
   constexpr int kGroup = 8 * kAtOnce;                  // ... that a wave scores together
-  __shared__ int s_bins[256];
+  __shared__ __attribute__((aligned(16))) int s_bins[2][256];  // of this digit, and of the next
   __shared__ int s_wave[2][kSelectWaves];
   __shared__ int s_pick[3];
   __shared__ uint32_t s_ticket;
@@ -110,6 +110,7 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = blockIdx.y, b = blockIdx.z;
+  if (tid < 256) s_bins[0][tid] = 0;
   const size_t bh = (size_t)b * a.kv_heads + h;
   const int len = clampi(a.ctx_lens[b], 0, a.max_len), P = 1 << a.page_shift;
   const int since = clampi(a.since != nullptr ? a.since[b] : a.ctx_lens[b] - 1, 0, len);
@@ -282,30 +283,26 @@ __global__ __launch_bounds__(kSelectThreads) void select_kernel(const SelectArgs
   uint32_t found = 0;    // digits of the budget-th largest key so far
   int above = 0;         // keys above all that begin so
   bool all = false;      // ... and those are listed too
-  for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-    if (tid < 256) s_bins[tid] = 0;
-    __syncthreads();
+  for (int shift = 24, buffer = 0; shift >= 0 && !all; shift -= 8, buffer ^= 1) {
     const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
     each([&](int, uint32_t key) {
-      if (key != 0u && (key & mask) == found) atomicAdd(&s_bins[key >> shift & 255u], 1);
+      if (key != 0u && (key & mask) == found) atomicAdd(&s_bins[buffer][key >> shift & 255u], 1);
     });
     __syncthreads();
-    // bins from the top: thread t has bin 255 - t
-    int n = 0, incl = 0;
-    if (wave < 4) {
-      n = s_bins[255 - tid];
-      incl = wave_inclusive_scan(n);
-      if (lane == 63) s_wave[0][wave] = incl;
-    }
-    __syncthreads();
-    if (wave < 4) {
-      int before = above;
-      for (int w = 0; w < wave; ++w) before += s_wave[0][w];
-      if (before + incl >= a.budget && before + incl - n < a.budget) {
-        s_pick[0] = 255 - tid;
-        s_pick[1] = before + incl - n;
-        s_pick[2] = before + incl == a.budget;
+    if (wave == 0) {  // bins from the top: lane l has 255 - 4 l and the three below
+      const i32x4 n = *reinterpret_cast<const i32x4*>(&s_bins[buffer][252 - 4 * lane]);
+      int before = above + wave_inclusive_scan(n[0] + n[1] + n[2] + n[3]) - (n[0] + n[1] + n[2] + n[3]);
+#pragma unroll
+      for (int k = 3; k >= 0; --k) {
+        if (before < a.budget && before + n[k] >= a.budget) {
+          s_pick[0] = 252 - 4 * lane + k;
+          s_pick[1] = before;
+          s_pick[2] = before + n[k] == a.budget;
+        }
+        before += n[k];
       }
+    } else if (tid < 64 + 256) {
+      s_bins[buffer ^ 1][tid - 64] = 0;
     }
     __syncthreads();
     found |= (uint32_t)s_pick[0] << shift;
