@@ -256,7 +256,7 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
       if (kFp4 && !is_q) {
         if (turned) turn_exactly<Elt, kPaired, false>(g, f, o);
         uint32_t exponent = block_exponent<kPer>(f);  // (a block's lanes are all here)
-        if (turned && exponent == kFp4LeastExponent + 127) {
+        if (turned && exponent <= kFp4LeastExponent + 128) {  // (from the next exponent on the least border, a quarter, is one of fp32's numbers of 24 bits)
           Elt::unpack(x[i], f);
           turn_exactly<Elt, kPaired, true>(g, f, o);
         }

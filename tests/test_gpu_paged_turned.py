@@ -252,6 +252,29 @@ def test_turned_values_next_to_borders(gpu_device):
     assert differ >= 16  # (rounded to fp32 first, as many rows would be others)
 
 
+@pytest.mark.parametrize("exponent", [-126, -125, -124, -110, 0, 125])
+def test_turned_values_next_to_borders_of_any_size(exponent, gpu_device):
+    """The same in blocks whose values, or borders, fp32 holds with fewer bits than 24 or not at all."""
+    D, n = 64, 16
+    angles, x = torch.zeros((n, 32)), torch.zeros((n, 1, D))
+    for t in range(n):
+        border = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0][t % 7]
+        x[t, 0, 0], x[t, 0, 16], x[t, 0, 1] = border, (-1.0) ** (t // 7) * 2.0 ** -10, 6.0
+        angles[t, :16], angles[t, 16:] = 1.0, 2.0 ** -20
+    x = (x.double() * 2.0 ** exponent).float()  # (exact: 2^-10 * 2^-126 is a multiple of 2^-149)
+    K, V = (span.fp4_pages(1, 1, 16, D, gpu_device) for _ in range(2))
+    table = torch.zeros((1, 1), dtype=torch.int32, device=gpu_device)
+    ctx, off = torch.tensor([n], dtype=torch.int32, device=gpu_device), torch.tensor([0, n], dtype=torch.int32, device=gpu_device)
+    xg = x.to(gpu_device)
+    span.paged_append_fp4(xg, xg, K, V, table, ctx, off, rotation=angles.to(gpu_device))
+    flat = K.cpu().reshape(-1).numpy()
+    for t in range(n):
+        code, byte = to_fp4(turned(x[t].double().numpy(), angles, t, False)[0])
+        codes, exps = place(16, D, t, False)
+        assert np.array_equal(flat[exps], byte[0]) and byte[0][0] == exponent + 127, t
+        assert np.array_equal(flat[codes], code[0][0::2] | (code[0][1::2] << 4)), t
+
+
 def test_fp4_beyond_four_gib(gpu_device):
     """Pages whose bytes lie past 32 bits."""
     N, KV, P, D = 66000, 8, 128, 128
