@@ -366,10 +366,10 @@ int64_t chunks_of(const span_paged_desc_t* d, int64_t rows, int loads) {
 struct TokenGrid {
   dim3 grid, block;
 };
-// Grid of so many waves a token; false: more than it holds.
+// Grid of so many waves a token; false: 2^32 lanes or more.
 bool grid_of(const span_paged_desc_t* d, int64_t chunks, int waves, TokenGrid* g) {
   const int64_t groups = ((int64_t)d->num_tokens + waves - 1) / waves * chunks;
-  if (groups * waves > 0x7fffffff) return false;
+  if (groups * waves > 0x3ffffff) return false;
   g->grid = dim3((unsigned)groups);
   g->block = dim3((unsigned)(64 * waves));
   return true;

@@ -96,6 +96,14 @@ def test_more_tokens_than_a_grid_holds():
     assert call("paged_read_fp4", d, *[FAR] * 7) == -2
 
 
+def test_more_waves_than_a_launch_numbers():
+    """2^32 lanes: rows of 2^26 tokens take a wave each at least."""
+    d = desc(heads=1, kv_heads=1, batch=1, dtype_code=1, num_tokens=(1 << 26) + 1)
+    assert call("paged_append_rotary", d, turn(), *[FAR] * 11) == -2
+    assert call("paged_append_fp4", d, turn(), *[FAR] * 10) == -2
+    assert call("paged_read_fp4", d, *[FAR] * 7) == -2
+
+
 @pytest.mark.parametrize("budget,sinks,recent,good", [(0, 0, 0, False), (1, 0, 0, True), (1, 0, 1, True), (1, 0, 2, False), (2, 0, 2, True), (2, 0, 17, True), (2, 0, 18, False),
                                                       (2, 1, 1, True), (2, 16, 1, True), (2, 17, 1, False), (3, 17, 1, True), (1 << 30, (1 << 31) - 1, (1 << 31) - 1, True)])
 def test_what_always_stays_has_to_fit_the_list(budget, sinks, recent, good):
