@@ -1,4 +1,12 @@
 // New rows into the pages with K (and q) turned by the angles of their positions, as they are or in 4 bits, and rows of 4-bit pages back as values.
+//
+// A pair of channels (x, x') becomes (x cos - x' sin, x sin + x' cos).  A wave takes a chunk of one token's rows, all of them of K, V and q in one launch; the rows are asked for first, and meanwhile
+// the token's sequence, position, angles and page are found.  A lane's pieces of 16 bytes are at the same channels of every row, so that its angles are loaded once; the other channel of a pair
+// comes from the lane that has it.
+// What bounds it: memory where there are many rows.  Prompts of 16 sequences (32 + 2 * 8 rows of 128 channels a token, bf16, 517 MB read and written): 102 us, 5.07 TB/s, which is what a copy of 1 GiB
+// reaches on the same card (5.06).  64 rows of a step: 4.4 us, a launch's least with a chain of three trips (length, page and angles, stores).
+// In 4 bits: 6 prompts, 2 * 32 rows of 128 a token, fp16: 52 us for 258 MB (half of which are the rows, whose nibbles leave in lines of 64 bytes that several tokens share), 21 us to read them
+// back; 64 rows of a step 4.6 and 3.4 us.
 #include "paged_device.h"
 
 namespace spanattn {
@@ -35,7 +43,9 @@ struct ReadArgs : TokenArgs {
   int32_t kv_heads, chunks;
 };
 
-// A wave takes a chunk of so many pieces of 16 bytes per lane of one token's rows; a workgroup's waves the same chunk of neighbouring tokens, or neighbouring chunks.
+// A wave takes a chunk of so many pieces of 16 bytes per lane of one token's rows; a workgroup's waves the same chunk of neighbouring tokens, or neighbouring chunks.  Two a lane for a few tokens (more waves), twelve for
+// many, the loads of a whole chunk under way together (with streamed stores and the other channel's values from their lane: the prompts above 121 -> 102 us); in 4 bits 2, 6 and 8 in place of four, or 4
+// and 8 waves in place of sixteen (100 us when each wave stored by itself), were no faster.
 constexpr int kFewLoads = 2, kManyLoads = 12, kFp4Loads = 4;
 constexpr int kWaves = 4, kFp4Waves = 16;  // (sixteen tokens' rows of 4-bit values fill their lines together, in one L2)
 constexpr int32_t kManyTokens = 512;

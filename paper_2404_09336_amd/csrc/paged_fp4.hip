@@ -8,10 +8,14 @@
 //     such a digit is an fp6 value (E2M3) exactly.  (The matrix core adds eight neighbouring products up with some 13 bits below the largest, measured; products of digits fit that, those of
 //     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block, fp32's six 25.
 //   * V becomes bf16, exactly, times its exponent: one instruction for two channels.  Weights meet it as three bf16 terms, all 24 bits.  (Two rounded terms leave 2^-18 of a weight, and outputs
-//     2.4e-6 off in place of 2e-7, for 1 to 3 % of a call.)
+//     2.4e-6 off in place of 1.4e-7, for 2 to 5 % of a call.)
 //   * A step of 32 positions is bound by the instructions that a SIMD issues, not by the matrix core, and few heads leave columns free.  With up to 8 heads a head has two columns,
 //     for even and odd channels: its weights go to every other of the product's inner places, zeros between them, and two channels of a row, as the conversion leaves them, need not be parted.  With up to 4
 //     heads it has four, and two terms go through one product.
+// What bounds it: memory where caches are even and large, else the start (launch, table entry, first rows: 5 us), the instructions of a SIMD's waves and the hand-over (3 us).  us, bytes over time: 64 x 8 pairs
+// of 512 .. 4096 positions, four heads of 128 each, bf16 (166 MB) 37, 4.5 TB/s, where slices of unlike length leave the longest to end alone (as many positions in level lengths, uncut: 30.5); 4 x 8 of
+// 8000 .. 32768 (83 MB) 21.7, 3.8 TB/s; 16 x 32 pairs of one head, ~500 positions in five spans, fp16 (42 MB) 13.4 .. 14.6; four heads of 64 and 256 positions, fp32, 4.85.
+// Heads of 64 channels fill half of a product with K: 71 MB in 25 us.
 #include "paged_attend.h"
 
 namespace spanattn {
@@ -27,7 +31,8 @@ typedef const SPAN_GLOBAL uint32_t* global_u32;
 constexpr int kUnitRows = kFp4Rows;
 constexpr int kStepUnits = 2;                  // units that a wave takes together: 32 positions of one product with V
 constexpr int kStepRows = kUnitRows * kStepUnits;
-// The reference of the weights is moved on when a score's weight would pass 2^kSlack (fp32 holds those as exactly).  Whenever the maximum moves: 57 instructions more in most of a wave's first steps.
+// The reference of the weights is moved on when a score's weight would pass 2^kSlack, not whenever the maximum moves: that is 57 instructions more in most of a wave's first steps.  (fp32 holds weights of 2^16 as exactly
+// as those below 1, and a sum of 2^31 of them.)
 constexpr float kSlack = 16.f;
 constexpr int kHeldUnits = 64;                 // of a wave, found at a time: one per lane
 
