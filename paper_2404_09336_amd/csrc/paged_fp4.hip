@@ -6,7 +6,7 @@
 //     time, and every load is contiguous over the wave.  Where a window, a span or the cache begins or ends inside a unit, its other rows are masked; two intervals that meet in a unit are two units.
 //   * K stays as it is: fp4 x fp6 products with both exponents applied by the matrix core.  q is laid out as kDigits digits to the base 16, each -16 .. 16 times a power of two that 32 channels share:
 //     such a digit is an fp6 value (E2M3) exactly.  (The matrix core adds eight neighbouring products up with some 13 bits below the largest, measured; products of digits fit that, those of
-//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block, fp32's six 25.
+//     floating values of different size do not.)  Five digits hold 21 bits below the largest channel of a block, six (fp32, or heads of 64) 25; of q below 2^-107 fewer.
 //   * V becomes bf16, exactly, times its exponent: one instruction for two channels.  Weights meet it as three bf16 terms, all 24 bits.  (Two rounded terms leave 2^-18 of a weight, and outputs
 //     2.4e-6 off in place of 1.4e-7, for 2 to 5 % of a call.)
 //   * A step of 32 positions is bound by the instructions that a SIMD issues, not by the matrix core, and few heads leave columns free.  With up to 8 heads a head has two columns,
@@ -14,8 +14,9 @@
 //     heads it has four, and two terms go through one product.
 // What bounds it: memory where caches are even and large, else the start (launch, table entry, first rows: 5 us), the instructions of a SIMD's waves and the hand-over (3 us).  us, bytes over time: 64 x 8 pairs
 // of 512 .. 4096 positions, four heads of 128 each, bf16 (166 MB) 37, 4.5 TB/s, where slices of unlike length leave the longest to end alone (as many positions in level lengths, uncut: 30.5); 4 x 8 of
-// 8000 .. 32768 (83 MB) 21.7, 3.8 TB/s; 16 x 32 pairs of one head, ~500 positions in five spans, fp16 (42 MB) 13.4 .. 14.6; four heads of 64 and 256 positions, fp32, 4.85.
-// Heads of 64 channels fill half of a product with K: 71 MB in 25 us.
+// 8000 .. 32768 (83 MB) 21.7, 3.8 TB/s; 16 x 32 pairs of one head, ~500 positions in five spans, fp16 (42 MB) 13.4 .. 14.6; four heads of 64 and 256 positions, fp32, 4.66.
+// Heads of 64 channels: two digits share a product with K, each half of the lanes has the rows (batch 27.7 -> 27.0, with fp32 queries 30.6 -> 29.2, the smallest call 4.88 -> 4.66; one digit and half a product of zeros
+// before).  The rest of a step is as long as for 128.
 #include "paged_attend.h"
 
 namespace spanattn {
@@ -36,8 +37,8 @@ constexpr int kStepRows = kUnitRows * kStepUnits;
 constexpr float kSlack = 16.f;
 constexpr int kHeldUnits = 64;                 // of a wave, found at a time: one per lane
 
-template <class Elt>
-constexpr int kDigitsOf = Elt::kBytes == 4 ? 6 : 5;
+template <class Elt, int D>
+constexpr int kDigitsOf = Elt::kBytes == 4 || D == 64 ? 6 : 5;
 
 // Units of a dense call: those of the first `sinks` positions, then those from `low` on.
 struct SeenUnits {
@@ -70,14 +71,14 @@ __device__ __forceinline__ uint32_t unit_mask(int u, int from, int to) {
 // q in LDS: of each head and block of 32 channels the fp6 codes of every digit, and the digits' exponent bytes (of digit t byte t).
 template <class Elt, int D>
 struct DigitTables {
-  uint32_t codes[kDigitsOf<Elt>][16][D / 32][6];
+  uint32_t codes[kDigitsOf<Elt, D>][16][D / 32][6];
   uint8_t exps[16][D / 32][8];
 };
 
 // What a thread loads for its (block, digit) number i ...
 template <class Elt, int D>
 struct QueryBlock {
-  static constexpr int kDigits = kDigitsOf<Elt>;
+  static constexpr int kDigits = kDigitsOf<Elt, D>;
   u32x4 piece[2 * Elt::kBytes];
   __device__ __forceinline__ void load(const PagedArgs& a, size_t row0, int i) {
     const int block = i % (D / 32), j = i / (D / 32 * kDigits);
@@ -145,7 +146,8 @@ constexpr int kFp4WavesPerSimd = D == 128 && kShare == 1 ? 3 : 4;
 template <class Elt, int D, PagedKind kKind, int kShare, class Args>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4WavesPerSimd<D, kShare>, kFp4WavesPerSimd<D, kShare>))) void fp4_kernel(const Args a) {
   constexpr bool kSpans = kKind == kPagedSpans;
-  constexpr int kDigits = kDigitsOf<Elt>;
+  constexpr int kDigits = kDigitsOf<Elt, D>;
+  constexpr int kProducts = D == 128 ? kDigits : kDigits / 2;  // of 128 inner places: one digit's channels, or two digits' 64
   constexpr int NE = D / 16;              // V channels of a lane
   constexpr int kHeads = 16 / kShare;     // heads that the columns hold
   constexpr int kSums = kShare == 1 ? NE : NE / 2;
@@ -357,29 +359,43 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
 #pragma unroll
     for (int s = 0; s < kStepUnits; ++s) sc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
     i32x8 digit[2];
-    auto read_digit = [&](int t, i32x8& to) {
+    auto read_digit = [&](int t, i32x8& to) {  // of product t
       asm volatile("" ::: "memory");
 #pragma unroll
-      for (int w = 0; w < 6; ++w) to[w] = (int)s_u.q.codes[t][q_row][q_block][w];
+      for (int w = 0; w < 6; ++w) to[w] = (int)s_u.q.codes[D == 128 ? t : 2 * t + c4 / 2][q_row][q_block][w];
       to[6] = to[7] = 0;
     };
-    read_digit(kDigits - 1, digit[(kDigits - 1) & 1]);
+    // (64: both halves of the lanes get a unit's rows, to meet a digit each)
+    u32x4 rows[kStepUnits];
+    uint32_t row_exps[kStepUnits];
+    if constexpr (D == 128) {
 #pragma unroll
-    for (int t = kDigits - 1; t >= 0; --t) {
+      for (int s = 0; s < kStepUnits; ++s) rows[s] = kr[kAt][s], row_exps[s] = ke[kAt][s];
+    } else {
+      auto both = [](uint32_t x, uint32_t& low, uint32_t& high) {
+        const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        low = r[0];
+        high = r[1];
+      };
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t low, high;
+        both(kr[kAt][0][w], low, high);
+        rows[0][w] = low;
+        rows[1][w] = high;
+      }
+      both(ke[kAt][0], row_exps[0], row_exps[1]);
+    }
+    read_digit(kProducts - 1, digit[(kProducts - 1) & 1]);
+#pragma unroll
+    for (int t = kProducts - 1; t >= 0; --t) {
       if (t > 0) read_digit(t - 1, digit[(t - 1) & 1]);
 #pragma unroll
       for (int s = 0; s < kStepUnits; ++s) {
         i32x8 k = {0, 0, 0, 0, 0, 0, 0, 0};
-        uint32_t e = ke[kAt][D == 128 ? s : 0];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) k[w] = (int)kr[kAt][D == 128 ? s : 0][w];
-        if constexpr (D == 64) {  // the other unit's lanes: zeros
-          const bool here = (lane < 32) == (s == 0);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) k[w] = here ? k[w] : 0;
-          e = here ? e : 0u;
-        }
-        sc[s] = digit_product(k, (int)e, digit[t & 1], q_exps, t, sc[s]);
+        for (int w = 0; w < 4; ++w) k[w] = (int)rows[s][w];
+        sc[s] = digit_product(k, (int)row_exps[s], digit[t & 1], q_exps, t, sc[s]);
       }
     }
     bool plain = true;
@@ -500,6 +516,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
   }
   __syncthreads();
   q_exps = *reinterpret_cast<const u32x2*>(s_u.q.exps[q_row][q_block]);
+  if constexpr (D == 64) q_exps[0] = __builtin_amdgcn_perm(q_exps[1], q_exps[0], c4 < 2 ? 0x0c040200u : 0x0c050301u);  // of the lane's digits
   const int units = steps * kStepUnits;
   auto next_of = [&](int w) {
     const int next = w + kStepUnits;
