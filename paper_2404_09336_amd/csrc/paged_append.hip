@@ -44,10 +44,10 @@ struct ReadArgs : TokenArgs {
 };
 
 // A wave takes a chunk of so many pieces of 16 bytes per lane of one token's rows; a workgroup's waves the same chunk of neighbouring tokens, or neighbouring chunks.  Two a lane for a few tokens (more waves), twelve for
-// many, the loads of a whole chunk under way together (with streamed stores and the other channel's values from their lane: the prompts above 121 -> 102 us); in 4 bits 2, 6 and 8 in place of four, or 4
-// and 8 waves in place of sixteen (100 us when each wave stored by itself), were no faster.
+// many, the loads of a whole chunk under way together (with streamed stores and the other channel's values from their lane: the prompts above 121 -> 102 us); in 4 bits 2, 6 and 8 in place of four were
+// no faster, sixteen waves a workgroup slower (53.7 -> 50.7 us for 8133 tokens of 2 * 32 rows of 128, fp16: with more than 64 registers a CU holds one of sixteen).
 constexpr int kFewLoads = 2, kManyLoads = 12, kFp4Loads = 4;
-constexpr int kWaves = 4, kFp4Waves = 16;  // (sixteen tokens' rows of 4-bit values fill their lines together, in one L2)
+constexpr int kWaves = 4, kFp4Waves = 8;
 constexpr int32_t kManyTokens = 512;
 
 // The sequence of a token's row, its slot and true position; b < 0: it belongs to none.
@@ -212,11 +212,22 @@ template <class Elt, int D, bool kFp4, bool kPaired, int kLoads>
 __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(const TurnArgs a) {
   constexpr int kPer = Elt::kPerVec, kRow = D / kPer;  // pieces of a row
   constexpr int kChunk = 64 * kLoads;
+  // Many tokens' 4-bit rows go out by way of LDS, so that neighbouring lanes store what neighbouring tokens have in a line: 16 bytes of K, 4 of V where a row by itself is stored by 4 and 1 (those
+  // tokens 59.6 -> 53.7 us).
+  constexpr bool kStaged = kFp4 && kLoads == kFp4Loads;
+  constexpr int kTokenCodes = kChunk * kPer / 2, kTokenExps = kChunk * kPer / kFp4Block;  // bytes of a token's chunk
+  __shared__ __attribute__((aligned(16))) unsigned char s_codes[kStaged ? kFp4Waves : 1][kStaged ? kTokenCodes + 16 : 16];
+  __shared__ unsigned char s_exps[kStaged ? kFp4Waves : 1][kStaged ? kTokenExps + 4 : 4];
+  __shared__ int s_rows[kFp4Waves];  // of the pool that the tokens have, or -1
   const int lane = threadIdx.x & 63;
   const uint32_t chunks = (uint32_t)a.chunks, waves = blockDim.x >> 6, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const uint32_t unit = blockIdx.x * waves + wave;
   const int t = kFp4 ? (int)(blockIdx.x / chunks * waves + wave) : (int)(unit / chunks), c = kFp4 ? (int)(blockIdx.x % chunks) : (int)(unit % chunks);
-  if (t >= a.num_tokens) return;
+  if constexpr (kStaged) {
+    if (lane == 0) s_rows[wave] = -1;  // (until it is known: what returns ahead of the barrier's wait has no row)
+  } else {
+    if (t >= a.num_tokens) return;
+  }
   const int rows = 2 * a.kv_heads + (a.q != nullptr ? a.heads : 0), pieces = rows * kRow;
   const int first = c * kChunk + lane, piece = lane % kRow;
   // Row number `row` of a token: of K, of V or of q, where it begins.
@@ -248,6 +259,7 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
     const int at_row = c * kChunk < 2 * a.kv_heads * kRow ? token_row(a, tok) : -1;  // of the pool (a chunk of q needs none)
     const size_t page = (size_t)(max(at_row, 0) >> a.page_shift);
     const uint32_t page_rows = 1u << a.page_shift, in_page = (uint32_t)max(at_row, 0) & (page_rows - 1u);
+    if (kStaged && lane == 0) s_rows[wave] = at_row;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       if (!kWhole && c * kChunk + 64 * i >= pieces) break;
@@ -271,7 +283,12 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
           turn_exactly<Elt, kPaired, true>(g, f, o);
         }
         const uint32_t w = to_codes<kPer>(f, exponent);
-        if (at_row >= 0 && (kWhole || at < pieces)) {
+        if constexpr (kStaged) {
+          const int here = 64 * i + lane;
+          if constexpr (kPer == 8) *(uint32_t*)&s_codes[wave][4 * here] = w;
+          else *(uint16_t*)&s_codes[wave][2 * here] = (uint16_t)w;
+          if (here * kPer % kFp4Block == 0) s_exps[wave][here * kPer / kFp4Block] = (unsigned char)exponent;
+        } else if (at_row >= 0 && (kWhole || at < pieces)) {
           const uint32_t ch = (uint32_t)piece * kPer;
           unsigned char* to = (unsigned char*)(is_v ? a.v : a.k) + (page * (size_t)a.kv_heads + (size_t)h) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
           const uint32_t code = is_v ? code_at<D, true>(in_page, ch) : code_at<D, false>(in_page, ch);
@@ -300,8 +317,39 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
       }
     }
   };
-  if ((c + 1) * kChunk <= pieces) whole_or_part(std::true_type());
-  else whole_or_part(std::false_type());
+  if (!kStaged || t < a.num_tokens) {
+    if ((c + 1) * kChunk <= pieces) whole_or_part(std::true_type());
+    else whole_or_part(std::false_type());
+  }
+  if constexpr (kStaged) {
+    constexpr int kRows = kChunk / kRow, kBlocks = D / kFp4Block, w = D / 16;  // rows of the chunk; w: channels that V has of a row in one place
+    const int row0 = c * kRows, end = min(kRows, 2 * a.kv_heads - row0);       // (rows of q from there on)
+    if (end <= 0) return;
+    __syncthreads();
+    const uint32_t page_rows = 1u << a.page_shift;
+    auto head_of = [&](int at_row, int row) {  // where a row's (page, head) begins
+      const bool is_v = row >= a.kv_heads;
+      return (unsigned char*)(is_v ? a.v : a.k) + ((size_t)(at_row >> a.page_shift) * (size_t)a.kv_heads + (size_t)(is_v ? row - a.kv_heads : row)) * ((size_t)page_rows * (D / 2 + D / kFp4Block));
+    };
+    for (int i = (int)threadIdx.x; i < end * kBlocks * kFp4Waves; i += 64 * kFp4Waves) {
+      const int token = i % kFp4Waves, block = i / kFp4Waves % kBlocks, r = i / (kFp4Waves * kBlocks), row = row0 + r, at_row = s_rows[token];
+      if (at_row < 0) continue;
+      unsigned char* to = head_of(at_row, row);
+      const uint32_t in_page = (uint32_t)at_row & (page_rows - 1u);
+      to[exponent_at<D>(page_rows, in_page, (uint32_t)block * kFp4Block)] = s_exps[token][r * kBlocks + block];
+      if (row < a.kv_heads) *(u32x4*)(to + code_at<D, false>(in_page, (uint32_t)block * kFp4Block)) = *(const u32x4*)&s_codes[token][r * (D / 2) + block * (kFp4Block / 2)];
+    }
+    const int first_v = max(a.kv_heads - row0, 0);
+    for (int i = (int)threadIdx.x; i < (end - first_v) * 16 * kFp4Waves; i += 64 * kFp4Waves) {
+      const int token = i % 4 + i / 64 % (kFp4Waves / 4) * 4, part = i / 4 % 16, r = first_v + i / (16 * kFp4Waves), at_row = s_rows[token];
+      if (at_row < 0) continue;
+      const uint32_t in_page = (uint32_t)at_row & (page_rows - 1u);
+      unsigned char* to = head_of(at_row, row0 + r) + code_at<D, true>(in_page, (uint32_t)(part * w));
+      const unsigned char* from = &s_codes[token][r * (D / 2) + part * (w / 2)];
+      if constexpr (w == 8) *(uint32_t*)to = *(const uint32_t*)from;
+      else *(uint16_t*)to = *(const uint16_t*)from;
+    }
+  }
 }
 
 template <class Elt, int D>
@@ -428,7 +476,7 @@ int append_turned(const span_paged_desc_t* d, const paged_rotation_t* rotation, 
   TokenGrid grid;
   if (!grid_of(d, chunks, kFp4 && many ? kFp4Waves : kWaves, &grid)) return SPAN_ERR_SHAPE;
   a.chunks = (int32_t)chunks;
-  const bool paired = rotation && rotation->paired, d128 = d->head_dim == 128;
+  const bool paired = !rotation || rotation->paired, d128 = d->head_dim == 128;
   hipStream_t stream = (hipStream_t)d->stream;
   switch (d->dtype) {
     case SPAN_F32:
