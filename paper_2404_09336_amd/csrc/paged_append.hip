@@ -106,10 +106,16 @@ struct Angles {
     partner = (second ? -half : half) / kPer;
     const bool known = (uint32_t)position < (uint32_t)a.angle_rows;
     const float* row = a.angles + (size_t)(known ? position : 0) * (size_t)a.channels + first;
+    constexpr int kWide = kOwn < 4 ? kOwn : 4;  // (the table's rows are whole lines of 64 bytes, halves of 32)
+    typedef float Wide __attribute__((ext_vector_type(kWide)));
+    Wide c[kOwn / kWide], s[kOwn / kWide];
+#pragma unroll
+    for (int i = 0; i < kOwn / kWide; ++i) c[i] = *(const Wide*)(row + kWide * i), s[i] = *(const Wide*)(row + half + kWide * i);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      cosine[i] = known ? row[i] : NAN;
-      sine[i] = known ? (second || kPaired ? row[half + i] : -row[half + i]) : NAN;
+      const float sin = s[i / kWide][i % kWide];
+      cosine[i] = known ? c[i / kWide][i % kWide] : NAN;
+      sine[i] = known ? (second || kPaired ? sin : -sin) : NAN;
     }
   }
 };
@@ -162,21 +168,32 @@ __device__ __forceinline__ void turn_exactly(const Angles<Elt, kPaired>& g, floa
   }
 }
 
-// Exponent byte of the block of 32 channels that kLanes lanes hold together, by the largest magnitude (as bits: NaN above infinity above numbers).
+// The largest of the lanes that hold a block of 32 channels together, kPer each; values not below zero as bits (NaN above infinity above numbers).
 template <int kPer>
-__device__ __forceinline__ uint32_t block_exponent(const float* x) {
-  float largest = 0.f;  // (NaN stays)
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) largest = __builtin_elementwise_maximum(largest, fabsf(x[i]));
-  uint32_t most = __builtin_bit_cast(uint32_t, largest) & 0x7fffffffu;
+__device__ __forceinline__ uint32_t block_most(uint32_t most) {
   most = max(most, (uint32_t)dpp_i<0xB1>((int)most));            // quad_perm [1,0,3,2]
   most = max(most, (uint32_t)dpp_i<0x4E>((int)most));            // quad_perm [2,3,0,1]
   if (kPer == 4) most = max(most, (uint32_t)dpp_i<0x141>((int)most));  // row_half_mirror
+  return most;
+}
+// Exponent byte of a block by its largest magnitude.
+__device__ __forceinline__ uint32_t exponent_of(uint32_t most) {
   constexpr uint32_t kSeven = 0x00600000u;                       // mantissa of 7 = 1.75 * 2^2
   constexpr uint32_t kMost = ((uint32_t)(kFp4MostExponent + 2 + 127) << 23) | kSeven;
   if (most > kMost) return 255u;
   const int e = (int)(most >> 23) - 2 + ((most & 0x7fffffu) > kSeven ? 1 : 0);  // e + 127
   return (uint32_t)max(e, kFp4LeastExponent + 127);
+}
+template <int kPer>
+__device__ __forceinline__ float largest_of(const float* x) {  // (NaN stays)
+  float largest = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) largest = __builtin_elementwise_maximum(largest, fabsf(x[i]));
+  return fabsf(largest);
+}
+template <int kPer>
+__device__ __forceinline__ uint32_t block_exponent(const float* x) {
+  return exponent_of(block_most<kPer>(__builtin_bit_cast(uint32_t, largest_of<kPer>(x))));
 }
 
 // Codes of 4 kPairs / 2 ... values by a block's exponent, the first in the lowest four bits.  (The instruction takes the scale's exponent alone, rounds to the nearest, ties to the even code, and
@@ -253,6 +270,8 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
     g.partner = 0;
     const bool only_v = c * kChunk >= a.kv_heads * kRow && (c + 1) * kChunk <= 2 * a.kv_heads * kRow;
     if (a.channels > 0 && !only_v) g.load(a, tok.position, piece);
+    float most_angle = 0.f;  // ... times 2^-21
+    if (kFp4 && g.turned) most_angle = 0x1p-21f * __builtin_elementwise_maximum(largest_of<Angles<Elt, kPaired>::kOwn>(g.cosine), largest_of<Angles<Elt, kPaired>::kOwn>(g.sine));
     if (c == 0 && a.positions != nullptr && (uint32_t)tok.p < (uint32_t)a.max_len) {
       for (int h = lane; h < a.kv_heads; h += 64) a.positions[((size_t)tok.b * a.kv_heads + h) * (size_t)a.max_len + tok.p] = tok.position;
     }
@@ -276,13 +295,42 @@ __global__ __launch_bounds__(64 * (kFp4 ? kFp4Waves : kWaves)) void turn_kernel(
         Elt::unpack(other, o);
       }
       if (kFp4 && !is_q) {
-        if (turned) turn_exactly<Elt, kPaired, false>(g, f, o);
-        uint32_t exponent = block_exponent<kPer>(f);  // (a block's lanes are all here)
-        if (turned && exponent <= kFp4LeastExponent + 128) {  // (from the next exponent on the least border, a quarter, is one of fp32's numbers of 24 bits)
-          Elt::unpack(x[i], f);
-          turn_exactly<Elt, kPaired, true>(g, f, o);
+        uint32_t exponent, w;
+        bool sure = false;
+        if (a.channels > 0 && !only_v) {
+          // In fp32 the turned values are less than `off` away: two products and a sum of 2^-24 each, at most 3 of them, and 2 for the sums with `off`, times the largest x times the largest angle; 8 are
+          // taken.  Where all that may be has one exponent and one code, those are the exact values' too.
+          float y[kPer], low[kPer], high[kPer], off = 0.f;
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) y[k] = f[k];
+          bool within = true;
+          if (turned) {
+            off = largest_of<kPer>(f);
+            if constexpr (!kPaired) off = __builtin_elementwise_maximum(off, largest_of<kPer>(o));
+            off *= most_angle;
+            within = off >= 0x1p-100f && off <= 0x1p+100f;  // (of others, fp32's least numbers and overflow among them, nothing is said)
+            turn<Elt, kPaired>(g, y, o);
+          }
+          const float most = largest_of<kPer>(y);
+          const float least_most = within ? __builtin_elementwise_maximum(most - off, 0.f) : 0.f, most_most = within ? most + off : INFINITY;
+          exponent = exponent_of(block_most<kPer>(__builtin_bit_cast(uint32_t, most_most)));  // (a block's lanes are all here)
+          sure = exponent == exponent_of(block_most<kPer>(__builtin_bit_cast(uint32_t, least_most)));
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) low[k] = y[k] - off, high[k] = y[k] + off;
+          w = to_codes<kPer>(high, exponent);
+          sure = sure && w == to_codes<kPer>(low, exponent);
         }
-        const uint32_t w = to_codes<kPer>(f, exponent);
+        if (__builtin_amdgcn_ballot_w64(!sure) != 0) {
+#pragma unroll
+          for (int k = 0; k < Angles<Elt, kPaired>::kOwn; ++k) asm volatile("" : "+v"(g.cosine[k]), "+v"(g.sine[k]));  // (not kept as 64-bit numbers beside)
+          if (turned) turn_exactly<Elt, kPaired, false>(g, f, o);
+          exponent = block_exponent<kPer>(f);
+          if (turned && exponent <= kFp4LeastExponent + 128) {  // (from the next exponent on the least border, a quarter, is one of fp32's numbers of 24 bits)
+            Elt::unpack(x[i], f);
+            turn_exactly<Elt, kPaired, true>(g, f, o);
+          }
+          w = to_codes<kPer>(f, exponent);
+        }
         if constexpr (kStaged) {
           const int here = 64 * i + lane;
           if constexpr (kPer == 8) *(uint32_t*)&s_codes[wave][4 * here] = w;
