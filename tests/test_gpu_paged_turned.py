@@ -10,6 +10,7 @@ from paged_reference import DTYPES, Pages
 pytestmark = pytest.mark.gpu
 
 LENS = [5, 16, 17, 100, 64, 1, 90, 3]
+MANY_LENS, MANY = [5, 200, 170, 33, 260, 1, 90, 3], [5, 187, 170, 33, 155, 1, 0, 7]  # more tokens than a step's: the kernels for those take longer chunks
 NEW = {"one": [1] * 8, "some": [5, 0, 1, 70, 33, 1, 20, 7]}  # (the last has 7 new tokens at 3 positions)
 
 
@@ -60,8 +61,18 @@ def within(got, want, size, dtype):
 @pytest.mark.parametrize("channels,paired", [(64, False), (64, True), (16, False), (48, True), (48, False)])
 @pytest.mark.parametrize("new", ["one", "some"])
 def test_rotary(dtype, heads, kv_heads, head_dim, channels, paired, new, gpu_device):
-    r = Rows(new, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels, ahead=30)
-    angles = rotation_table(300, channels)
+    check_rotary(Rows(new, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels, ahead=30), dtype, kv_heads, channels, paired, gpu_device)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(2, 1, 64), (9, 3, 128), (11, 11, 64)])
+@pytest.mark.parametrize("channels,paired", [(64, False), (64, True), (16, False), (48, True)])
+def test_rotary_of_many_tokens(dtype, heads, kv_heads, head_dim, channels, paired, gpu_device):
+    check_rotary(Rows(MANY, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels, ahead=30, lens=MANY_LENS), dtype, kv_heads, channels, paired, gpu_device)
+
+
+def check_rotary(r, dtype, kv_heads, channels, paired, gpu_device):
+    angles = rotation_table(500, channels)
     K, V, table, ctx = r.pages.to("K", "V", "table", "ctx")
     k, v, q, off, seen = r.on(gpu_device, "k", "v", "q", "off", "seen")
     positions = torch.full((8, kv_heads, r.pages.capacity), -9, dtype=torch.int32)
@@ -148,10 +159,21 @@ def test_a_full_table_drops_rows_and_turns_their_queries(gpu_device):
 @pytest.mark.parametrize("new", ["one", "some"])
 def test_fp4(dtype, heads, kv_heads, head_dim, channels, paired, new, gpu_device):
     """Every byte of the pools, the rows read back, and q."""
-    r = Rows(new, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels + 1, ahead=30)
+    check_fp4(Rows(new, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels + 1, ahead=30), dtype, kv_heads, head_dim, channels, paired, gpu_device)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(2, 1, 64), (9, 3, 128), (11, 11, 64), (18, 18, 128)])
+@pytest.mark.parametrize("channels,paired", [(0, False), (64, False), (64, True), (48, False), (16, True)])
+def test_fp4_of_many_tokens(dtype, heads, kv_heads, head_dim, channels, paired, gpu_device):
+    r = Rows(MANY, heads, kv_heads, head_dim, dtype, gpu_device, seed=channels + 1, ahead=30, lens=MANY_LENS)
+    check_fp4(r, dtype, kv_heads, head_dim, channels, paired, gpu_device)
+
+
+def check_fp4(r, dtype, kv_heads, head_dim, channels, paired, gpu_device):
     scale = 2.0 ** torch.randint(-8, 9, (*r.k.shape[:2], head_dim // 32), generator=r.pages.generator).repeat_interleave(32, -1)
     r.k, r.v = (r.k * scale).to(r.k.dtype), (r.v * scale).to(r.k.dtype)
-    angles = rotation_table(300, channels) if channels else None
+    angles = rotation_table(500, channels) if channels else None
     N, row_bytes = r.pages.K.shape[0], head_dim // 2 + head_dim // 32
     g = torch.Generator().manual_seed(3)
     pools = [torch.randint(0, 256, (N, kv_heads, 16, row_bytes), generator=g).to(torch.uint8) for _ in range(2)]
@@ -250,6 +272,36 @@ def test_turned_values_next_to_borders(gpu_device):
         assert np.array_equal(rows[0][t].cpu().double().numpy(), want), t
         differ += not np.array_equal(want, from_fp4(*to_fp4(y.astype(np.float32))))
     assert differ >= 16  # (rounded to fp32 first, as many rows would be others)
+
+
+@pytest.mark.parametrize("paired", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_turned_values_next_to_borders_of_many_tokens(dtype, paired, gpu_device):
+    """Values that are a few units of fp32 and less from a border, or on it, between others of every size; blocks whose largest value is next to where the exponent changes."""
+    D, n, C = 128, 640, 64
+    g = torch.Generator().manual_seed(8)
+    x = torch.randn((n, 2, D), generator=g) * 2.0 ** torch.randint(-20, 21, (n, 2, 1), generator=g)
+    angles = rotation_table(n, C)
+    one = [2 * i for i in range(32)] if paired else list(range(32))
+    two = [2 * i + 1 for i in range(32)] if paired else list(range(32, 64))
+    for t in range(0, n, 2):  # angle 0 and almost: x cos - x' sin = border + j tiny
+        angles[t, :32], angles[t, 32:] = 1.0, 2.0 ** -18
+        for i in range(32):
+            x[t, 0, one[i]] = [0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0][(t // 2 + i) % 8] * (1 if i % 3 else -1)
+            x[t, 0, two[i]] = float(torch.randint(-3, 4, (1,), generator=g)) * 2.0 ** -(6 + t % 16)
+    x = x.to(DTYPES[dtype])
+    K, V = (span.fp4_pages(40, 2, 16, D, gpu_device) for _ in range(2))
+    table = torch.arange(40, dtype=torch.int32, device=gpu_device)[None].contiguous()
+    ctx, off = torch.tensor([n], dtype=torch.int32, device=gpu_device), torch.tensor([0, n], dtype=torch.int32, device=gpu_device)
+    xg = x.to(gpu_device)
+    span.paged_append_fp4(xg, xg, K, V, table, ctx, off, rotation=angles.to(gpu_device), paired=paired)
+    flat = K.cpu().reshape(40, 2, -1).numpy()
+    for t in range(n):
+        code, byte = to_fp4(turned(x[t].double().numpy(), angles, t, paired)[0])
+        codes, exps = place(16, D, t % 16, False)
+        for h in range(2):
+            assert np.array_equal(flat[t // 16, h][exps], byte[h]), (t, h)
+            assert np.array_equal(flat[t // 16, h][codes], code[h][0::2] | (code[h][1::2] << 4)), (t, h)
 
 
 @pytest.mark.parametrize("exponent", [-126, -125, -124, -110, 0, 125])
