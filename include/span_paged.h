@@ -136,7 +136,7 @@ int paged_append_rotary(const span_paged_desc_t* desc, const paged_rotation_t* r
  */
 
 /* paged_append into such pools, K (and q) turned on the way as by paged_append_rotary if rotation is not NULL.  K is turned in 64 bits and rounded once.  Without
- * rotation q and q_out have to be NULL. */
+ * rotation rows of q go into q_out as they are. */
 int paged_append_fp4(const span_paged_desc_t* desc, const paged_rotation_t* rotation, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
                      const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, const int32_t* seen, const void* q, void* q_out);
 

@@ -499,7 +499,6 @@ int append_turned(const span_paged_desc_t* d, const paged_rotation_t* rotation, 
   rc = check_rotation(d, rotation);
   if (rc != SPAN_OK) return rc;
   if (!q != !q_out) return SPAN_ERR_NULL;
-  if (q && !rotation) return SPAN_ERR_SHAPE;
   if (!q_offsets && d->num_tokens != 0 && d->num_tokens != d->batch) return SPAN_ERR_SHAPE;
   if (d->num_tokens == 0) return SPAN_OK;
   if (!k_new || !v_new || !k || !v || !block_table || !ctx_lens) return SPAN_ERR_NULL;

@@ -321,15 +321,13 @@ def _rotation(rotation, paired, head_dim, device):
     return _Rotation(rotation.data_ptr(), int(rotation.shape[0]), int(rotation.shape[1]), int(bool(paired)))
 
 
-def _turned_queries(q, q_out, rotation, T, kv_heads, head_dim, dtype, stream, device):
+def _turned_queries(q, q_out, T, kv_heads, head_dim, dtype, stream, device):
     """(heads, q_out): heads is kv_heads where no q comes along."""
     import torch
     if q is None:
         if q_out is not None:
             raise ValueError("q_out needs q")
         return kv_heads, None
-    if rotation is None:
-        raise ValueError("q is turned along with K: it needs rotation")
     if q.dim() != 3:
         raise ValueError("expected q [num_tokens, heads, head_dim]")
     _on_gpu(q, "q", dtype, (T, q.shape[1], head_dim), device)
@@ -355,7 +353,7 @@ def _prepare_append(name, k_new, v_new, k_pages, v_pages, block_table, ctx_lens,
     if q_offsets is None and T != B:
         raise ValueError("without q_offsets there is one new token per sequence")
     turn = _rotation(rotation, paired, D, device)
-    H, q_out = _turned_queries(q, q_out, rotation, T, KV, D, dtype, stream, device)
+    H, q_out = _turned_queries(q, q_out, T, KV, D, dtype, stream, device)
     opt = lambda t, name, shape: None if t is None else _on_gpu(t, name, torch.int32, shape, device)  # noqa: E731
     offsets, positions_ptr, seen_ptr = opt(q_offsets, "q_offsets", (B + 1,)), opt(positions, "positions", (B, KV, TP * P)), opt(seen, "seen", (B,))
     desc = make_paged_desc(B, H, KV, D, _dtype_code(k_new), P, N, TP, num_tokens=T, stream=_stream(stream, device))
@@ -385,7 +383,7 @@ def paged_append_rotary(k_new, v_new, k_pages, v_pages, block_table, ctx_lens, r
 
 def prepare_paged_append_fp4(k_new, v_new, k_pages, v_pages, block_table, ctx_lens, q_offsets=None, *, rotation=None, paired=False, q=None, q_out=None,
                              seen=None, stream=None) -> PreparedCall:
-    """Into pools of 4-bit values (fp4_pages), turned if rotation is given: see prepare_paged_append_rotary."""
+    """Into pools of 4-bit values (fp4_pages), turned if rotation is given (otherwise q goes into q_out as it is): see prepare_paged_append_rotary."""
     return _prepare_append("paged_append_fp4", k_new, v_new, k_pages, v_pages, block_table, ctx_lens, rotation, q_offsets, paired, q, q_out, None, seen, stream)
 
 

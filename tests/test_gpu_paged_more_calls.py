@@ -103,7 +103,7 @@ def test_refused_arguments(gpu_device):
     s = Setting(gpu_device)
     half = s.prompt[2][:, :, :32].contiguous()
     calls = [lambda: span.paged_decode_attn_fp4(s.q.double(), s.K4, s.V4, s.table, s.ctx, 1.0), lambda: s.decode(window=-1), lambda: s.decode(sinks=1 << 31),
-             lambda: span.paged_append_fp4(*s.new, s.K4, s.V4, s.table, s.ctx, q=s.q), lambda: span.paged_append_fp4(*s.new, s.K4, s.V4, s.table, s.ctx, s.offsets[:3]),
+             lambda: span.paged_append_fp4(*s.new, s.K4, s.V4, s.table, s.ctx, q_out=s.q), lambda: span.paged_append_fp4(*s.new, s.K4, s.V4, s.table, s.ctx, s.offsets[:3]),
              lambda: span.paged_append_rotary(*s.new, s.K, s.V, s.table, s.ctx, None), lambda: span.paged_append_rotary(*s.new, s.K, s.V, s.table, s.ctx, s.rotation[:, :24].contiguous()),
              lambda: span.paged_append_rotary(*s.new, s.K, s.V, s.table, s.ctx, s.rotation, q_out=s.q), lambda: s.rotary(q_out=half), lambda: s.rotary(q_out=s.prompt[2].float()),
              lambda: span.paged_append_rotary(*s.prompt[:2], s.K, s.V, s.table, s.ctx, s.rotation), lambda: span.paged_read_fp4(s.K4, s.V4, s.table, s.ctx, k_rows=s.rows[0], v_rows=s.rows[1]),

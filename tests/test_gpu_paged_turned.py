@@ -274,6 +274,26 @@ def test_turned_values_next_to_borders(gpu_device):
     assert differ >= 16  # (rounded to fp32 first, as many rows would be others)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv_heads,head_dim", [(2, 1, 64), (9, 3, 128)])
+@pytest.mark.parametrize("new", ["some", MANY])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_queries_without_rotation(dtype, heads, kv_heads, head_dim, new, in_place, gpu_device):
+    """They pass through, those of dropped rows too; nobody's are left alone; the pools are those of a call without q."""
+    r = Rows(new, heads, kv_heads, head_dim, dtype, gpu_device, lens=MANY_LENS if new is MANY else LENS)
+    table, ctx = r.pages.to("table", "ctx")
+    k, v, q, off = r.on(gpu_device, "k", "v", "q", "off")
+    q_out = q if in_place else torch.full_like(q, 7.0)
+    pools = [[span.fp4_pages(r.pages.K.shape[0], kv_heads, 16, head_dim, gpu_device) for _ in range(2)] for _ in range(2)]
+    span.paged_append_fp4(k, v, *pools[0], table, ctx, off)
+    got = span.paged_append_fp4(k, v, *pools[1], table, ctx, off, q=q, q_out=q_out)
+    assert len(got) == 3 and got[2] is q_out and all(same(a, b) for a, b in zip(*pools))
+    rows = [row for row, *_ in r.tokens]
+    want = r.q.clone() if in_place else torch.full_like(r.q, 7.0)
+    want[rows] = r.q[rows]
+    assert same(q_out.cpu(), want)
+
+
 @pytest.mark.parametrize("paired", [False, True])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_turned_values_next_to_borders_of_many_tokens(dtype, paired, gpu_device):
