@@ -3,10 +3,10 @@
 // A pair of channels (x, x') becomes (x cos - x' sin, x sin + x' cos).  A wave takes a chunk of one token's rows, all of them of K, V and q in one launch; the rows are asked for first, and meanwhile
 // the token's sequence, position, angles and page are found.  A lane's pieces of 16 bytes are at the same channels of every row, so that its angles are loaded once; the other channel of a pair
 // comes from the lane that has it.
-// What bounds it: memory where there are many rows.  Prompts of 16 sequences (32 + 2 * 8 rows of 128 channels a token, bf16, 517 MB read and written): 102 us, 5.07 TB/s, which is what a copy of 1 GiB
-// reaches on the same card (5.06).  64 rows of a step: 4.4 us, a launch's least with a chain of three trips (length, page and angles, stores).
-// In 4 bits: 6 prompts, 2 * 32 rows of 128 a token, fp16: 52 us for 258 MB (half of which are the rows, whose nibbles leave in lines of 64 bytes that several tokens share), 21 us to read them
-// back; 64 rows of a step 4.6 and 3.4 us.
+// What bounds it: memory where there are many rows.  Prompts of 16 sequences (32 + 2 * 8 rows of 128 channels a token, bf16, 517 MB read and written): 94.7 us, 5.5 TB/s, where a copy of 1 GiB
+// reaches 5.06 on the same card.  64 rows of a step: 4.2 us, a launch's least with a chain of three trips (length, page and angles, stores).
+// In 4 bits: 6 prompts, 2 * 32 rows of 128 a token, fp16: 47 us for 165 MB, 3.5 TB/s, 21 us to read them back; 64 rows of a step 4.6 and 3.4 us.  What is between 47 and the 33 of memory: waves that all find
+// their token, wait for angles and page and only then convert, with 4 to 6 of them on a SIMD (registers).
 #include "paged_device.h"
 
 namespace spanattn {
@@ -106,7 +106,8 @@ struct Angles {
     partner = (second ? -half : half) / kPer;
     const bool known = (uint32_t)position < (uint32_t)a.angle_rows;
     const float* row = a.angles + (size_t)(known ? position : 0) * (size_t)a.channels + first;
-    constexpr int kWide = kOwn < 4 ? kOwn : 4;  // (the table's rows are whole lines of 64 bytes, halves of 32)
+    // (the table's rows are whole lines of 64 bytes, halves of 32; one number at a time took 102 us in place of 95 for the prompts above, in 4 bits 80 in place of 60 for 8133 tokens turned by halves)
+    constexpr int kWide = kOwn < 4 ? kOwn : 4;
     typedef float Wide __attribute__((ext_vector_type(kWide)));
     Wide c[kOwn / kWide], s[kOwn / kWide];
 #pragma unroll
