@@ -11,7 +11,7 @@ struct PagedArgs : LaunchArgs {  // heads: KV heads; max_len: positions of a seq
   int32_t table_pages, page_shift, num_pages;
   int32_t group;             // query heads per KV head
   int32_t batch, window, sinks;
-  int32_t room, more_room;   // > 0: slices per head aimed at, see locate_slice; 0: num_splits each, or the table
+  int32_t room, more_room;   // > 0: slices per head aimed at, see slice_length, and rows of the grid; 0: num_splits each, or the table
   int32_t whole;             // up to so many positions a sequence is not cut
   int32_t least;             // positions of a slice at least
   float* scores;             // [batch, kv head, query head of the group, max_len] unscaled scores by virtual position, or null
@@ -48,13 +48,7 @@ struct Slice {
   int b, split, nsl, y0, len;  // sequence, slice within it, slices of it, slot of its first slice; its length (locate_slice)
 };
 
-// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than `whole`, T whole steps and
-// PagedArgs::least at least; row y of the grid is the y-th of them.  T starts at the positions of all sequences over `room` and grows, by the slices too
-// many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice well above the
-// mean, which is what the whole call waits for then, `more_room` is tried.  Every workgroup works it out for itself: one load of the lengths,
-// which it needs anyway, and a few scans for up to 64 sequences.
-// (us, 1024 workgroups always -> 512 and 1024 where those are not level: 32 sequences in a window of 1024 29.0 -> 27.0, four of 8000 .. 32768 72.9 -> 68.7;
-// 512 always: 64 x 8 pairs of 512 .. 4096 106.4 -> 112.2.  One round each way: with as many slices as came out, 1.25 rounds, those took 110.9.)
+// The slice that row y of the grid is (slice_length).  Every workgroup works it out for itself: one load of the lengths, which it needs anyway, and a few scans for up to 64 sequences.
 // count_of(length): positions that a sequence of so many attends.
 template <class CountOf>
 __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lane, CountOf&& count_of) {
@@ -69,31 +63,15 @@ __device__ __forceinline__ Slice locate_slice(const PagedArgs& a, int y, int lan
     all += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(n), 63);
     longest = max(longest, (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_max(n), 63));
   }
-  auto steps = [](uint32_t x) { return (x + kPagedSliceStep - 1u) / kPagedSliceStep * kPagedSliceStep; };
   auto slices = [&](uint32_t T) { return n > a.whole ? (int)(((uint32_t)n + T - 1u) / T) : 1; };  // of this lane's sequence
-  const uint32_t batch = (uint32_t)a.batch;
-  uint32_t T = longest;
-  if (longest > (uint32_t)a.whole) {
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {
-      const uint32_t room = (uint32_t)(pass == 0 ? a.room : a.more_room);
-      T = longest;
-      if (room > batch) {
-        const float mean = (float)all / ((float)room - 0.5f * (float)batch);  // (a sequence has half a slice more than its share on average)
-        T = max(steps((uint32_t)mean), (uint32_t)a.least);
-        while (T < longest) {
-          uint32_t total = 0;
-          for (int c = 0; c < a.batch; c += 64) {
-            if (a.batch > 64) fetch(c);
-            total += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(c + lane < a.batch ? slices(T) : 0), 63);
-          }
-          if (total <= room) break;
-          T = min(max(steps((uint32_t)((float)T * (float)total / (float)room)), steps(T + T / 16)), longest);
-        }
-      }
-      if ((float)min(T, longest) * (float)max(room, batch) <= 1.4f * (float)all || T <= (uint32_t)a.least) break;
+  const uint32_t T = slice_length(all, longest, (uint32_t)a.batch, (uint32_t)a.room, (uint32_t)a.more_room, (uint32_t)a.whole, (uint32_t)a.least, [&](uint32_t T) {  // of all
+    uint32_t total = 0;
+    for (int c = 0; c < a.batch; c += 64) {
+      if (a.batch > 64) fetch(c);
+      total += (uint32_t)__builtin_amdgcn_readlane(wave_inclusive_scan(c + lane < a.batch ? slices(T) : 0), 63);
     }
-  }
+    return total;
+  });
   Slice s = {-1, 0, 1, 0, 0};
   int before = 0;
   for (int c = 0; c < a.batch; c += 64) {

@@ -42,18 +42,5 @@ __device__ __forceinline__ int sequence_of(const int32_t* offsets, int batch, in
   }
 }
 
-// Positions that the token at position n - 1 sees: [0, sinks) and from `low` on, of those below n that the table has.
-struct Seen {
-  int sinks, low, count;
-};
-__device__ __forceinline__ Seen seen_by_last(int n, int max_len, int window, int sinks) {
-  const int held = clampi(n, 0, max_len);
-  Seen s;
-  s.low = window > 0 ? clampi(max(n, 0) - window, 0, held) : 0;
-  s.sinks = min(sinks, s.low);
-  s.count = held - s.low + s.sinks;
-  return s;
-}
-
 }  // namespace spanattn
 #endif

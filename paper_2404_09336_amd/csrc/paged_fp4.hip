@@ -40,18 +40,6 @@ constexpr int kHeldUnits = 64;                 // of a wave, found at a time: on
 template <class Elt, int D>
 constexpr int kDigitsOf = Elt::kBytes == 4 || D == 64 ? 6 : 5;
 
-// Units of a dense call: those of the first `sinks` positions, then those from `low` on.
-struct SeenUnits {
-  int sinks, low, held, first;  // positions; units of the sinks
-};
-__device__ __forceinline__ SeenUnits seen_units(const PagedArgs& a, int len) {
-  const Seen s = seen_by_last(len, a.max_len, a.window, a.sinks);
-  return SeenUnits{s.sinks, s.low, clampi(len, 0, a.max_len), (s.sinks + kUnitRows - 1) / kUnitRows};
-}
-__device__ __forceinline__ int unit_count(const SeenUnits& s) {
-  return s.first + (s.held > s.low ? (s.held + kUnitRows - 1) / kUnitRows - s.low / kUnitRows : 0);
-}
-
 // Units of an interval [start, end) of a span list: none if it is empty.
 __device__ __forceinline__ int interval_units(const PagedArgs& a, int start, int end, int& from, int& to) {
   from = clampi(start, 0, a.max_len);
@@ -173,7 +161,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
     sl = Slice{(int)(entry & 1023u), (int)(entry >> 10 & 2047u), (int)(entry >> 21), 0, 0};
     sl.y0 = (int)blockIdx.y - sl.split;
   } else if (!kSpans && a.room > 0) {
-    sl = locate_slice(a, (int)blockIdx.y, lane, [&](int len) { return unit_count(seen_units(a, len)) * kUnitRows; });
+    sl = locate_slice(a, (int)blockIdx.y, lane, [&](int len) { return unit_count(seen_units(len, a.max_len, a.window, a.sinks)) * kUnitRows; });
     if (sl.b < 0) return;  // (the grid holds the most slices that any lengths give)
   } else {
     sl.nsl = a.num_splits;
@@ -213,7 +201,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
     }
   } else {
     if (a.room == 0) sl.len = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]);
-    seen = seen_units(a, sl.len);
+    seen = seen_units(sl.len, a.max_len, a.window, a.sinks);
     all = unit_count(seen);
   }
   all = __builtin_amdgcn_readfirstlane(all);

@@ -56,7 +56,8 @@ PagedPlan plan_paged(const span_paged_desc_t* d, PagedKind kind, uint32_t* table
     if (most <= whole) return uniform(1);
     p.room = (int32_t)room;
     p.splits = 2;
-    p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(most, least) * d->batch));
+    const int64_t held = fp4 ? most_unit_positions(cap, d->window, d->sinks) : most;  // as the kernel counts them
+    p.rows = (int32_t)std::max<int64_t>(d->batch, std::min<int64_t>(more_room, ceil_div(held, least) * d->batch));
     p.cut = more_room > d->batch;  // (otherwise one slice each whatever the lengths; the workspace is that of other batches of the shape)
     p.own_weights = !p.cut && most * d->batch * d->kv_heads <= kPagedOwnWeights;
     return p;

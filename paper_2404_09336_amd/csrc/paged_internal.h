@@ -17,6 +17,19 @@ constexpr int kPagedLocateBatch = 512;
 // What a one-token call attends: the cache up to a token (window, sinks), a sequence's span, or the pages listed for a (sequence, KV head).
 enum PagedKind { kPagedDense, kPagedSpans, kPagedSelected };
 
+// What host and device count alike (constexpr: code of both).
+constexpr int within(int x, int lo, int hi) { return x < lo ? lo : (x > hi ? hi : x); }
+
+// Positions that the token at position n - 1 sees: [0, sinks) and from `low` on, of those below n that the table has.
+struct Seen {
+  int sinks, low, count;
+};
+constexpr Seen seen_by_last(int n, int max_len, int window, int sinks) {
+  const int held = within(n, 0, max_len), low = window > 0 ? within((n > 0 ? n : 0) - window, 0, held) : 0;
+  const int first = sinks < low ? sinks : low;
+  return Seen{first, low, held - low + first};
+}
+
 // A sequence of up to so many positions is not cut: the hand-over costs more than a workgroup's two or four tiles a wave.
 inline int32_t paged_whole(const span_paged_desc_t* d, bool fp4 = false) { return fp4 ? 1024 : d->dtype == SPAN_F32 && d->head_dim == 128 ? 128 : 256; }
 // Rows of 4 bits are through four times as fast, and a hand-over (some 3.5 us) costs as much as a thousand of them.  us, 256 positions at least and whole up to 256 -> 512 and 1024: 16 x 32
@@ -75,6 +88,56 @@ int check_rotation(const span_paged_desc_t* d, const paged_rotation_t* r);
 constexpr int kFp4Rows = 16, kFp4Block = 32;  // rows of a group, channels that share an exponent
 constexpr int kFp4LeastExponent = -126, kFp4MostExponent = 125;
 inline int64_t fp4_page_bytes(const span_paged_desc_t* d) { return (int64_t)d->page_size * (d->head_dim / 2 + d->head_dim / kFp4Block); }
+
+// A one-token call over such pages goes by units, a group's rows: those of the first `sinks` positions, then those from `low` on.  A unit that both touch is two.
+struct SeenUnits {
+  int sinks, low, held, first;  // positions; units of the sinks
+};
+constexpr SeenUnits seen_units(int n, int max_len, int window, int sinks) {
+  const Seen s = seen_by_last(n, max_len, window, sinks);
+  return SeenUnits{s.sinks, s.low, within(n, 0, max_len), (s.sinks + kFp4Rows - 1) / kFp4Rows};
+}
+constexpr int unit_count(const SeenUnits& s) { return s.first + (s.held > s.low ? (s.held + kFp4Rows - 1) / kFp4Rows - s.low / kFp4Rows : 0); }
+// Positions of the most units that any length has: W positions in a row touch (W + 14) / 16 + 1 of them at most, and of a table's units the one where sinks end and the window begins can be there twice.
+constexpr int64_t most_unit_positions(int64_t max_len, int64_t window, int64_t sinks) {
+  if (window <= 0) return max_len;
+  const int64_t units = (sinks + kFp4Rows - 1) / kFp4Rows + (window + kFp4Rows - 2) / kFp4Rows + 1, table = max_len / kFp4Rows + (sinks > 0 ? 1 : 0);
+  return (units < table ? units : table) * kFp4Rows;
+}
+
+// Slices of a dense call: sequence b has one, or ceil(n_b / T) of at most T positions if it has more than `whole`, T whole steps and `least` at least.  T starts at the positions of all
+// sequences over `room` and grows, by the slices too many in proportion and a sixteenth at least, until no more than `room` are left or no sequence is cut.  If that leaves the longest slice
+// well above the mean, which is what the whole call waits for then, `rows` is tried.  More than `rows`, the slices that the grid and the workspace hold, it never gives: a bound of them that is
+// too low costs time and nothing else.
+// (us, 1024 workgroups always -> 512 and 1024 where those are not level: 32 sequences in a window of 1024 29.0 -> 27.0, four of 8000 .. 32768 72.9 -> 68.7;
+// 512 always: 64 x 8 pairs of 512 .. 4096 106.4 -> 112.2.  One round each way: with as many slices as came out, 1.25 rounds, those took 110.9.)
+// `all`, `longest`: positions of the sequences; slices(T): all their slices of that length.
+template <class Slices>
+constexpr __attribute__((always_inline)) uint32_t slice_length(uint32_t all, uint32_t longest, uint32_t batch, uint32_t room, uint32_t rows, uint32_t whole, uint32_t least, Slices&& slices) {
+  constexpr uint32_t kStep = kPagedSliceStep;
+  uint32_t T = longest;
+  if (longest <= whole) return T;
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    const uint32_t aim = pass == 0 ? room : rows, most = aim < rows ? aim : rows;
+    T = longest;
+    if (most > batch) {
+      const float mean = (float)all / ((float)aim - 0.5f * (float)batch);  // (a sequence has half a slice more than its share on average)
+      T = ((uint32_t)mean + kStep - 1u) / kStep * kStep;
+      if (T < least) T = least;
+      while (T < longest) {
+        const uint32_t total = slices(T);
+        if (total <= most) break;
+        const uint32_t in_proportion = ((uint32_t)((float)T * (float)total / (float)most) + kStep - 1u) / kStep * kStep, sixteenth = (T + T / 16 + kStep - 1u) / kStep * kStep;
+        T = in_proportion > sixteenth ? in_proportion : sixteenth;
+        if (T > longest) T = longest;
+      }
+    }
+    const float longest_slice = (float)(T < longest ? T : longest);
+    if (longest_slice * (float)(aim > batch ? aim : batch) <= 1.4f * (float)all || T <= least) break;
+  }
+  return T;
+}
 
 // A selection's scores, one of each page of a (sequence, KV head), behind the counters.
 int check_select(const span_paged_desc_t* d);
