@@ -35,6 +35,9 @@ constexpr int kStepRows = kUnitRows * kStepUnits;
 // The reference of the weights is moved on when a score's weight would pass 2^kSlack, not whenever the maximum moves: that is 57 instructions more in most of a wave's first steps.  (fp32 holds weights of 2^16 as exactly
 // as those below 1, and a sum of 2^31 of them.)
 constexpr float kSlack = 16.f;
+// A page holds values up to 6 * 2^125, and up to 2^22 weights of 2^16 each would take a sum past fp32 whose mean is within.  From a wave's first block of V with an exponent of 65 or more on its
+// weights stay 2^kLower below: 2^(16 - 40 + 22) of the largest values, and of those ahead 2^(16 + 22) below 2^68, are less than 2^126.  (What is below 2^-86 beside such a block loses bits.)
+constexpr float kLower = 40.f;
 constexpr int kHeldUnits = 64;                 // of a wave, found at a time: one per lane
 
 template <class Elt, int D>
@@ -271,6 +274,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
 
   // A weight is exp2(score * post + shift): what the state is relative to is -shift as it is, rounded, and not the score that it came from.
   float shift = INFINITY, lsum = 0.f;
+  bool large = false;  // a block of V that asks for kLower has been here
   // Unnormalised outputs.  kShare 1: O[e][r] of column qi's head, channel NE (4 c4 + r) + e.  Otherwise O[p][r], channel NE (4 c4 + r) + 2 p + odd; kShare 4: the term's part of it.
   f32x4 O[kSums];
 #pragma unroll
@@ -406,9 +410,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kFp4Wa
 #pragma unroll
       for (int r = 0; r < 4; ++r) mx = fmaxf(mx, sc[s][r]);
     }
-    if (__builtin_amdgcn_ballot_w64(fmaf(mx, post, shift) > kSlack) != 0) {
+    const uint32_t upper_bits = (Ve[0] & Ve[0] << 1 | Ve[1] & Ve[1] << 1) & 0x80808080u;  // of an exponent byte from 192 on both
+    large = large || __builtin_amdgcn_ballot_w64(upper_bits != 0u) != 0;
+    const float lower = large ? kLower : 0.f;
+    if (__builtin_amdgcn_ballot_w64(fmaf(mx, post, shift) > kSlack - lower) != 0) {
       mx = across_groups_max<16>(mx);
-      const float to = fminf(shift, -(mx * post)), to_safe = to == INFINITY ? 0.f : to;
+      const float to = fminf(shift, -(mx * post) - lower), to_safe = to == INFINITY ? 0.f : to;
       const float alpha = __builtin_amdgcn_exp2f(to_safe - shift);
       shift = to;
       lsum *= alpha;
