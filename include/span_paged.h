@@ -117,6 +117,9 @@ typedef struct paged_rotation {
  *   y_i = x_i cos - x_i' sin        y_i' = x_i sin + x_i' cos        in fp32, rounded once; channels past rotation->channels stay
  * Where the table has no position t the turned channels become NaN.  A row of q is turned also where its row of K is dropped; rows of
  * tokens of no sequence are left alone.
+ * Calls of 2^26 waves or more are refused with SPAN_ERR_SHAPE.  A token takes one for each started 12 KiB of its rows of K, V and q (paged_append_fp4: 4 KiB; 2 KiB in both
+ * where num_tokens is below 512; paged_read_fp4: 4 KiB of K and V), num_tokens is rounded up to four (4-bit calls from 512 tokens on: eight).  With 8 KV heads and 32 query
+ * heads of 128, 16 bits, that is some 67 million tokens, in 4 bits 22 million.
  */
 int paged_append_rotary(const span_paged_desc_t* desc, const paged_rotation_t* rotation, const void* k_new, const void* v_new, void* k_pages,
                         void* v_pages, const int32_t* block_table, const int32_t* ctx_lens, const int32_t* q_offsets, int32_t* positions,
