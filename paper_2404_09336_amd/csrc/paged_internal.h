@@ -87,7 +87,6 @@ int check_rotation(const span_paged_desc_t* d, const paged_rotation_t* r);
 // each by sixteenths of the channels and in those by rows, the exponents by blocks and in each by rows: what a lane of the attention kernel takes is contiguous.
 constexpr int kFp4Rows = 16, kFp4Block = 32;  // rows of a group, channels that share an exponent
 constexpr int kFp4LeastExponent = -126, kFp4MostExponent = 125;
-inline int64_t fp4_page_bytes(const span_paged_desc_t* d) { return (int64_t)d->page_size * (d->head_dim / 2 + d->head_dim / kFp4Block); }
 
 // A one-token call over such pages goes by units, a group's rows: those of the first `sinks` positions, then those from `low` on.  A unit that both touch is two.
 struct SeenUnits {
