@@ -5,8 +5,9 @@
 // comes from the lane that has it.
 // What bounds it: memory where there are many rows.  Prompts of 16 sequences (32 + 2 * 8 rows of 128 channels a token, bf16, 517 MB read and written): 94.7 us, 5.5 TB/s, where a copy of 1 GiB
 // reaches 5.06 on the same card.  64 rows of a step: 4.2 us, a launch's least with a chain of three trips (length, page and angles, stores).
-// In 4 bits: 6 prompts, 2 * 32 rows of 128 a token, fp16: 47 us for 165 MB, 3.5 TB/s, 21 us to read them back; 64 rows of a step 4.6 and 3.4 us.  What is between 47 and the 33 of memory: waves that all find
-// their token, wait for angles and page and only then convert, with 4 to 6 of them on a SIMD (registers).
+// In 4 bits: 6 prompts, 5675 tokens of 2 * 32 rows of 128 and 32 of q, half of the channels turned in pairs, fp16 (211 MB read and written): 46 .. 47 us, 4.5 TB/s, where 41 are a copy's; 60 with all of
+// them turned by halves; 21 .. 22 us to read them back (118 MB).  8133 such tokens without q (169 MB, a copy's 33): 44 turned in pairs or not at all, 57.5 by halves.  What is between: waves that all find their
+// token, wait for angles and page and only then convert, 4 to 6 on a SIMD; those by halves have the other channels' values and both bounds of the error in registers too.  64 rows of a step 4.6 and 3.4 us.
 #include "paged_device.h"
 
 namespace spanattn {

@@ -13,8 +13,9 @@
 //     for even and odd channels: its weights go to every other of the product's inner places, zeros between them, and two channels of a row, as the conversion leaves them, need not be parted.  With up to 4
 //     heads it has four, and two terms go through one product.
 // What bounds it: memory where caches are even and large, else the start (launch, table entry, first rows: 5 us), the instructions of a SIMD's waves and the hand-over (3 us).  us, bytes over time: 64 x 8 pairs
-// of 512 .. 4096 positions, four heads of 128 each, bf16 (166 MB) 37, 4.5 TB/s, where slices of unlike length leave the longest to end alone (as many positions in level lengths, uncut: 30.5); 4 x 8 of
-// 8000 .. 32768 (83 MB) 21.6 .. 22.2, 3.8 TB/s; 16 x 32 pairs of one head, ~500 positions in five spans, fp16 (42 MB) 13.4 .. 15.5; four heads of 64 and 256 positions, fp32, 4.66.
+// of 512 .. 4096 positions, four heads of 128 each, bf16 (166 MB, each byte fetched once) 37 .. 38, 4.4 TB/s, where slices of unlike length leave the longest to end alone (as many positions in level lengths, uncut: 30.5);
+// 32 x 8 in a window of 4096 with 4 sinks (143 MB) 31 .. 32, 4.5 TB/s, 64 x 8 in one of 2048 28.7, 5.0 TB/s; 4 x 8 of 8000 .. 32768 (83 MB) 22.0 .. 22.5, 3.7 TB/s; 16 x 32 pairs of one head, ~500 positions in
+// five spans, fp16 (42 MB, 49 fetched) 14.4 .. 15.4; four heads of 64 and 256 positions, fp32, 4.8; one sequence's 8 pairs in a window of 4096 10.9.
 // Heads of 64 channels: two digits share a product with K, each half of the lanes has the rows (batch 27.7 -> 27.0, with fp32 queries 30.6 -> 29.2, the smallest call 4.88 -> 4.66; one digit and half a product of zeros
 // before).  The rest of a step is as long as for 128.
 #include "paged_attend.h"

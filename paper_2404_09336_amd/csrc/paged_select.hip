@@ -4,7 +4,7 @@
 // scores stay in LDS, otherwise the workgroup that is done last for its pair (a ticket) fetches them; it finds the budget-th largest by digits and lists what lies above, in order.
 // Scores are summed in 64 bits and rounded once, so that pages rank the same however their sums are split; what is equal after that ranks by page.
 // What bounds it: memory, 2 * head_dim values of bounds a page, and behind it some 7 us of a launch, the first trips and the selection.  64 x 8 pairs of 2000 .. 8192 positions in pages of 16, four query heads
-// each, fp16 (85 MB): 21.8 us; twice the pages take 13 more, 6.5 TB/s.  The bounds of 4 x 8 prompts of 8000 .. 32768 in pages of 64, bf16 (161 MB of K): 37.5 us, of which the rows take 28.
+// each, fp16 (85 MB): 21.8 us; twice the pages take 13 more, 6.5 TB/s.  The bounds of 4 x 8 prompts of 8000 .. 32768 in pages of 64, bf16 (156 MB of K): 37.5 us, of which the rows take 28.
 // Digits of 8 bits: four rounds of counting at most, fewer where a digit ends with the list full, two barriers each.
 #include <algorithm>
 
